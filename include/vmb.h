@@ -412,6 +412,208 @@ vmb_status vmb_ss2d_out_norm(const void* y, const void* z, const float* gamma, c
                              float eps, void* out, int64_t batch, int64_t channels, int64_t P,
                              vmb_dtype dtype, vmb_stream_t stream);
 
+/*
+ * Gated delta rule: a linear recurrence over tokens like the selective scan
+ * above, with a matrix state and an error-correcting write. Per sequence and
+ * value head h, which reads key head h / (heads_v / heads_k):
+ *   S'  = exp(g_t) S_{t-1}                         (S: dk x dv, binary32)
+ *   e_t = v_t - S'^T k_t
+ *   S_t = S' + beta_t k_t e_t^T
+ *   o_t = scale S_t^T q_t
+ * The forward and backward calls take whole sequences in chunks of tokens on
+ * the matrix cores: binary32 accumulation, inputs of type float32 and every
+ * computed operand as sums of two or three bfloat16 values (two, about 16
+ * bits, where all outputs of the call are bfloat16).
+ *
+ *   q, k : dtype, [batch, L, heads_k, dk]; v : dtype, [batch, L, heads_v, dv].
+ *          A token's heads are contiguous; tokens are q_stride, k_stride,
+ *          v_stride elements apart (batch rows L times that), so that the
+ *          three may be views of one projection's output. A head's keys are
+ *          expected to have a length of at most about 1 (beta |k|^2 <= 2 keeps
+ *          the recurrence from growing); any finite values are computed.
+ *   g    : float32, [batch, L, heads_v], log decays (at most 0 for a decaying
+ *          state; below -128, and -inf, the decay is 0)
+ *   beta : float32, [batch, L, heads_v]
+ *   h0   : float32, [n_seq, heads_v, dk, dv], or NULL (zeros)
+ *   cu_seqlens : int32, [n_seq + 1] (device), or NULL. NULL: n_seq == batch
+ *          sequences of L tokens. Else batch == 1 and sequence s is tokens
+ *          cu_seqlens[s] .. cu_seqlens[s + 1] - 1 of the L packed ones (may be
+ *          empty; non-decreasing from 0 to L). The values are read on the
+ *          device: values outside that rule never lead out of the tensors,
+ *          but leave the tokens that no sequence holds unwritten.
+ *   o    : dtype, [batch, L, heads_v, dv] (output)
+ *   hT   : float32, [n_seq, heads_v, dk, dv], the states after the last
+ *          tokens (output), or NULL
+ *   dk, dv : multiples of 8, dk <= 128, dv <= 256; heads_v a multiple of
+ *          heads_k; strides a multiple of 16 bytes
+ *   workspace : vmb_gated_delta_workspace_bytes(0, ...) bytes, as for the scan
+ * Values that are not finite spread to the other tokens of their chunk (up to
+ * 64) in that head, earlier ones included, and to all later ones of their
+ * sequence; never to other sequences or heads.
+ * Errors: VMB_ERR_NULL, VMB_ERR_SHAPE (sizes, strides, n_seq, scale not
+ * finite), VMB_ERR_UNSUPPORTED (dk, dv), VMB_ERR_DTYPE, VMB_ERR_ALIGN (q, k, v,
+ * o and the states 16 bytes, g, beta and cu_seqlens 4), VMB_ERR_ALIAS,
+ * VMB_ERR_WORKSPACE.
+ */
+vmb_status vmb_gated_delta_fwd(const void* q, const void* k, const void* v, const float* g,
+                               const float* beta, const float* h0, const int32_t* cu_seqlens,
+                               void* o, float* hT, int64_t batch, int64_t L, int64_t n_seq,
+                               int64_t heads_k, int64_t heads_v, int64_t dk, int64_t dv,
+                               int64_t q_stride, int64_t k_stride, int64_t v_stride, float scale,
+                               vmb_dtype dtype, void* workspace, size_t workspace_bytes,
+                               vmb_stream_t stream);
+
+/*
+ * Gradients of vmb_gated_delta_fwd: inputs as there, with
+ *   d_o  : dtype, [batch, L, heads_v, dv], the gradient of o
+ *   d_hT : float32, [n_seq, heads_v, dk, dv], that of hT, or NULL (zeros)
+ * and outputs (all contiguous)
+ *   d_q, d_k : dtype, [batch, L, heads_k, dk] (summed over the value heads
+ *          that share a key head, in a fixed order)
+ *   d_v  : dtype, [batch, L, heads_v, dv]
+ *   d_g, d_beta : float32, [batch, L, heads_v] (d_g is 0 where the decay is)
+ *   d_h0 : float32, [n_seq, heads_v, dk, dv], or NULL
+ * The states are computed again from the inputs; nothing is kept from the
+ * forward call. Workspace vmb_gated_delta_workspace_bytes(1, ...).
+ * Errors as for vmb_gated_delta_fwd.
+ */
+vmb_status vmb_gated_delta_bwd(const void* q, const void* k, const void* v, const float* g,
+                               const float* beta, const float* h0, const int32_t* cu_seqlens,
+                               const void* d_o, const float* d_hT, void* d_q, void* d_k, void* d_v,
+                               float* d_g, float* d_beta, float* d_h0, int64_t batch, int64_t L,
+                               int64_t n_seq, int64_t heads_k, int64_t heads_v, int64_t dk,
+                               int64_t dv, int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                               float scale, vmb_dtype dtype, void* workspace,
+                               size_t workspace_bytes, vmb_stream_t stream);
+
+/*
+ * Bytes of device workspace of vmb_gated_delta_fwd (backward = 0) or
+ * vmb_gated_delta_bwd (backward = 1); SIZE_MAX for an invalid shape.
+ */
+size_t vmb_gated_delta_workspace_bytes(int backward, int64_t batch, int64_t L, int64_t n_seq,
+                                       int64_t heads_k, int64_t heads_v, int64_t dk, int64_t dv,
+                                       vmb_dtype dtype);
+
+/*
+ * The recurrence of vmb_gated_delta_fwd token by token on states that are
+ * kept between calls: row b of the batch takes its T tokens through state
+ * slots[b] of the pool, all in binary32.
+ *   q, k, v, g, beta, o : as there with L = T (o contiguous)
+ *   slots : int32, [batch] (device), or NULL (row b takes state b; then
+ *           n_slots >= batch). A row whose slot is negative or not below
+ *           n_slots is skipped: its o is set to 0 and no state is touched. No
+ *           two rows may name the same slot.
+ *   state : float32, [n_slots, heads_v, dk, dv]: read and written in place
+ * Errors as for vmb_gated_delta_fwd (no workspace).
+ */
+vmb_status vmb_gated_delta_step(const void* q, const void* k, const void* v, const float* g,
+                                const float* beta, const int32_t* slots, float* state, void* o,
+                                int64_t batch, int64_t T, int64_t n_slots, int64_t heads_k,
+                                int64_t heads_v, int64_t dk, int64_t dv, int64_t q_stride,
+                                int64_t k_stride, int64_t v_stride, float scale, vmb_dtype dtype,
+                                vmb_stream_t stream);
+
+/* Options of the rotary calls (bit flags). */
+typedef enum {
+    /* pair j is (x[2j], x[2j + 1]) of a head; without it (x[j], x[j + pairs]) */
+    VMB_ROTARY_INTERLEAVED = 1,
+    /* each head is divided by sqrt(sum of its squares + norm_eps) first */
+    VMB_ROTARY_NORM = 2
+} vmb_rotary_option;
+
+/*
+ * Rotary positions with several axes (row and column of an image token, time
+ * too for video): pair j of each head of token t turns by
+ *   theta = positions[b, t, axis(j)] * inv_freq[j],
+ *   (x1, x2) -> (x1 cos theta - x2 sin theta, x1 sin theta + x2 cos theta);
+ * the axes take sections[0], sections[1], ... consecutive pairs. Elements
+ * past the last pair pass unturned. With VMB_ROTARY_NORM the head is scaled to
+ * unit length first (over all dim elements). Angles are formed and reduced in
+ * binary64; the rest is binary32.
+ *   q : dtype, [batch, L, heads_q, dim], tokens q_stride elements apart (as
+ *       for the delta rule); k likewise with heads_k and k_stride, or NULL
+ *       (then yk NULL too)
+ *   positions : int32, [positions_batch, L, n_axes], positions_batch 1 (shared)
+ *       or batch
+ *   inv_freq  : float32, [pairs], pairs = the sum of the sections
+ *   sections  : HOST array of n_axes sizes >= 0, read during the call
+ *   yq, yk    : dtype, [batch, L, heads, dim], contiguous (outputs)
+ *   dim even, 2 <= dim <= 512, 1 <= pairs <= dim / 2, n_axes 1 to 4
+ * Errors: VMB_ERR_NULL, VMB_ERR_SHAPE, VMB_ERR_UNSUPPORTED (dim, n_axes, an
+ * unknown option), VMB_ERR_DTYPE, VMB_ERR_ALIGN (bases not aligned to their
+ * element), VMB_ERR_ALIAS.
+ */
+vmb_status vmb_axis_rotary_fwd(const void* q, const void* k, const int32_t* positions,
+                               const float* inv_freq, const int64_t* sections, void* yq, void* yk,
+                               int64_t batch, int64_t L, int64_t heads_q, int64_t heads_k,
+                               int64_t dim, int64_t n_axes, int64_t positions_batch,
+                               int64_t q_stride, int64_t k_stride, unsigned options,
+                               float norm_eps, vmb_dtype dtype, vmb_stream_t stream);
+
+/*
+ * Gradients of vmb_axis_rotary_fwd. d_yq, d_yk [batch, L, heads, dim] are those
+ * of its outputs, d_q, d_k (outputs) those of its inputs, all contiguous. q and
+ * k, with their strides, are read with VMB_ROTARY_NORM only (NULL without):
+ *   p = R^T dy,  dx = r (p - x (x . p) r^2),  r = 1 / sqrt(|x|^2 + norm_eps)
+ * or dx = R^T dy without the norm. d_yk NULL: no second tensor.
+ */
+vmb_status vmb_axis_rotary_bwd(const void* d_yq, const void* d_yk, const void* q, const void* k,
+                               const int32_t* positions, const float* inv_freq,
+                               const int64_t* sections, void* d_q, void* d_k, int64_t batch,
+                               int64_t L, int64_t heads_q, int64_t heads_k, int64_t dim,
+                               int64_t n_axes, int64_t positions_batch, int64_t q_stride,
+                               int64_t k_stride, unsigned options, float norm_eps, vmb_dtype dtype,
+                               vmb_stream_t stream);
+
+/* Activations of the group norm. */
+typedef enum {
+    VMB_ACT_NONE = 0, /* y = z                   */
+    VMB_ACT_SILU = 1  /* y = z / (1 + exp(-z))   */
+} vmb_act;
+
+/*
+ * Group norm with an activation on channels-last maps x [batch, P, channels]
+ * (P = H * W pixels); group j is channels j c .. (j + 1) c - 1 of all pixels of
+ * an image, c = channels / groups:
+ *   mean, var = those of the group's P c values (var biased),
+ *   rstd = 1 / sqrt(var + eps),  z = (x - mean) rstd gamma + beta,  y = act(z)
+ *   x, y : dtype, [batch, P, channels];  gamma, beta : float32, [channels] or
+ *          NULL (1 and 0);  mean, rstd : float32, [batch, groups] (outputs), or
+ *          both NULL
+ *   eps >= 0, finite;  workspace : vmb_group_norm_act_workspace_bytes(0, ...)
+ * Statistics in binary32: means and centred sums of squares of short runs,
+ * joined pairwise, so an offset of the values does not cost accuracy.
+ * Errors: VMB_ERR_NULL, VMB_ERR_SHAPE (sizes, channels not a multiple of
+ * groups, eps), VMB_ERR_UNSUPPORTED (act, more than 16384 channels),
+ * VMB_ERR_DTYPE, VMB_ERR_ALIGN (x, y, workspace 16 bytes; the rest 4),
+ * VMB_ERR_ALIAS, VMB_ERR_WORKSPACE.
+ */
+vmb_status vmb_group_norm_act_fwd(const void* x, const float* gamma, const float* beta, void* y,
+                                  float* mean, float* rstd, int64_t batch, int64_t P,
+                                  int64_t channels, int64_t groups, float eps, vmb_act act,
+                                  vmb_dtype dtype, void* workspace, size_t workspace_bytes,
+                                  vmb_stream_t stream);
+
+/*
+ * Gradients of vmb_group_norm_act_fwd from dy, the input x and the mean and
+ * rstd that the forward call wrote: dz = dy act'(z),
+ *   dgamma = sum over images and pixels of dz xhat,  dbeta = of dz,
+ *   dx = rstd (dz gamma - m1 - xhat m2), m1 and m2 the group means of
+ *   dz gamma and dz gamma xhat
+ *   dx : dtype, [batch, P, channels];  dgamma, dbeta : float32, [channels], or
+ *   both NULL. Sums in a fixed order. Errors as for the forward call.
+ */
+vmb_status vmb_group_norm_act_bwd(const void* dy, const void* x, const float* gamma,
+                                  const float* beta, const float* mean, const float* rstd,
+                                  void* dx, float* dgamma, float* dbeta, int64_t batch, int64_t P,
+                                  int64_t channels, int64_t groups, vmb_act act, vmb_dtype dtype,
+                                  void* workspace, size_t workspace_bytes, vmb_stream_t stream);
+
+/* Workspace of the group norm's calls (backward 0 or 1); SIZE_MAX for an
+ * invalid shape. */
+size_t vmb_group_norm_act_workspace_bytes(int backward, int64_t batch, int64_t P,
+                                          int64_t channels, int64_t groups);
+
 /* Static, NUL-terminated description of a status code. */
 const char* vmb_status_string(vmb_status s);
 

@@ -144,6 +144,120 @@ size_t vmb_scan_workspace_bytes(int mean_variant, int64_t batch, int64_t K, int6
     return scan_workspace_bytes(mean_variant, batch, K, channels, L, N, layout);
 }
 
+vmb_status vmb_gated_delta_fwd(const void* q, const void* k, const void* v, const float* g,
+                               const float* beta, const float* h0, const int32_t* cu_seqlens,
+                               void* o, float* hT, int64_t batch, int64_t L, int64_t n_seq,
+                               int64_t heads_k, int64_t heads_v, int64_t dk, int64_t dv,
+                               int64_t q_stride, int64_t k_stride, int64_t v_stride, float scale,
+                               vmb_dtype dtype, void* workspace, size_t workspace_bytes,
+                               vmb_stream_t stream) {
+    DeltaArgs a{};
+    a.q = q, a.k = k, a.v = v, a.g = g, a.beta = beta, a.h0 = h0, a.cu = cu_seqlens;
+    a.o = o, a.hT = hT;
+    a.batch = batch, a.L = L, a.n_seq = n_seq, a.heads_k = heads_k, a.heads_v = heads_v;
+    a.dk = dk, a.dv = dv, a.q_stride = q_stride, a.k_stride = k_stride, a.v_stride = v_stride;
+    a.scale = scale, a.dt = dtype, a.ws = workspace, a.ws_bytes = workspace_bytes;
+    a.stream = static_cast<hipStream_t>(stream);
+    const vmb_status st = validate_delta(a, false);
+    return st != VMB_OK ? st : launch_delta_fwd(a);
+}
+
+vmb_status vmb_gated_delta_bwd(const void* q, const void* k, const void* v, const float* g,
+                               const float* beta, const float* h0, const int32_t* cu_seqlens,
+                               const void* d_o, const float* d_hT, void* d_q, void* d_k, void* d_v,
+                               float* d_g, float* d_beta, float* d_h0, int64_t batch, int64_t L,
+                               int64_t n_seq, int64_t heads_k, int64_t heads_v, int64_t dk,
+                               int64_t dv, int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                               float scale, vmb_dtype dtype, void* workspace,
+                               size_t workspace_bytes, vmb_stream_t stream) {
+    DeltaArgs a{};
+    a.q = q, a.k = k, a.v = v, a.g = g, a.beta = beta, a.h0 = h0, a.cu = cu_seqlens;
+    a.d_o = d_o, a.d_hT = d_hT, a.d_q = d_q, a.d_k = d_k, a.d_v = d_v;
+    a.d_g = d_g, a.d_beta = d_beta, a.d_h0 = d_h0;
+    a.batch = batch, a.L = L, a.n_seq = n_seq, a.heads_k = heads_k, a.heads_v = heads_v;
+    a.dk = dk, a.dv = dv, a.q_stride = q_stride, a.k_stride = k_stride, a.v_stride = v_stride;
+    a.scale = scale, a.dt = dtype, a.ws = workspace, a.ws_bytes = workspace_bytes;
+    a.stream = static_cast<hipStream_t>(stream);
+    const vmb_status st = validate_delta(a, true);
+    return st != VMB_OK ? st : launch_delta_bwd(a);
+}
+
+size_t vmb_gated_delta_workspace_bytes(int backward, int64_t batch, int64_t L, int64_t n_seq,
+                                       int64_t heads_k, int64_t heads_v, int64_t dk, int64_t dv,
+                                       vmb_dtype dtype) {
+    return delta_workspace_bytes(backward != 0, batch, L, n_seq, heads_k, heads_v, dk, dv, dtype);
+}
+
+vmb_status vmb_gated_delta_step(const void* q, const void* k, const void* v, const float* g,
+                                const float* beta, const int32_t* slots, float* state, void* o,
+                                int64_t batch, int64_t T, int64_t n_slots, int64_t heads_k,
+                                int64_t heads_v, int64_t dk, int64_t dv, int64_t q_stride,
+                                int64_t k_stride, int64_t v_stride, float scale, vmb_dtype dtype,
+                                vmb_stream_t stream) {
+    const DeltaStepArgs a{q,       k,       v,  g,  beta,     slots,    state,    o,
+                          batch,   T,       n_slots, heads_k, heads_v, dk, dv, q_stride,
+                          k_stride, v_stride, scale, dtype, static_cast<hipStream_t>(stream)};
+    const vmb_status st = validate_delta_step(a);
+    return st != VMB_OK ? st : launch_delta_step(a);
+}
+
+vmb_status vmb_axis_rotary_fwd(const void* q, const void* k, const int32_t* positions,
+                               const float* inv_freq, const int64_t* sections, void* yq, void* yk,
+                               int64_t batch, int64_t L, int64_t heads_q, int64_t heads_k,
+                               int64_t dim, int64_t n_axes, int64_t positions_batch,
+                               int64_t q_stride, int64_t k_stride, unsigned options,
+                               float norm_eps, vmb_dtype dtype, vmb_stream_t stream) {
+    const RotaryArgs a{q, k, nullptr, nullptr, positions, inv_freq, sections, yq, yk, batch, L,
+                       heads_q, heads_k, dim, n_axes, positions_batch, q_stride, k_stride,
+                       options, norm_eps, dtype, static_cast<hipStream_t>(stream)};
+    const vmb_status st = validate_rotary(a, false);
+    return st != VMB_OK ? st : launch_rotary(a, false);
+}
+
+vmb_status vmb_axis_rotary_bwd(const void* d_yq, const void* d_yk, const void* q, const void* k,
+                               const int32_t* positions, const float* inv_freq,
+                               const int64_t* sections, void* d_q, void* d_k, int64_t batch,
+                               int64_t L, int64_t heads_q, int64_t heads_k, int64_t dim,
+                               int64_t n_axes, int64_t positions_batch, int64_t q_stride,
+                               int64_t k_stride, unsigned options, float norm_eps, vmb_dtype dtype,
+                               vmb_stream_t stream) {
+    const RotaryArgs a{d_yq, d_yk, q, k, positions, inv_freq, sections, d_q, d_k, batch, L,
+                       heads_q, heads_k, dim, n_axes, positions_batch, q_stride, k_stride,
+                       options, norm_eps, dtype, static_cast<hipStream_t>(stream)};
+    const vmb_status st = validate_rotary(a, true);
+    return st != VMB_OK ? st : launch_rotary(a, true);
+}
+
+vmb_status vmb_group_norm_act_fwd(const void* x, const float* gamma, const float* beta, void* y,
+                                  float* mean, float* rstd, int64_t batch, int64_t P,
+                                  int64_t channels, int64_t groups, float eps, vmb_act act,
+                                  vmb_dtype dtype, void* workspace, size_t workspace_bytes,
+                                  vmb_stream_t stream) {
+    const GroupNormArgs a{x, nullptr, gamma, beta, y, mean, rstd, nullptr, nullptr, batch, P,
+                          channels, groups, eps, act, dtype, workspace, workspace_bytes,
+                          static_cast<hipStream_t>(stream)};
+    const vmb_status st = validate_group_norm(a, false);
+    return st != VMB_OK ? st : launch_group_norm(a, false);
+}
+
+vmb_status vmb_group_norm_act_bwd(const void* dy, const void* x, const float* gamma,
+                                  const float* beta, const float* mean, const float* rstd,
+                                  void* dx, float* dgamma, float* dbeta, int64_t batch, int64_t P,
+                                  int64_t channels, int64_t groups, vmb_act act, vmb_dtype dtype,
+                                  void* workspace, size_t workspace_bytes, vmb_stream_t stream) {
+    const GroupNormArgs a{x, dy, gamma, beta, dx, const_cast<float*>(mean),
+                          const_cast<float*>(rstd), dgamma, dbeta, batch, P, channels, groups,
+                          0.0f, act, dtype, workspace, workspace_bytes,
+                          static_cast<hipStream_t>(stream)};
+    const vmb_status st = validate_group_norm(a, true);
+    return st != VMB_OK ? st : launch_group_norm(a, true);
+}
+
+size_t vmb_group_norm_act_workspace_bytes(int backward, int64_t batch, int64_t P,
+                                          int64_t channels, int64_t groups) {
+    return group_norm_workspace_bytes(backward != 0, batch, P, channels, groups);
+}
+
 vmb_status vmb_discrete_scan(const float* abar, const float* bu, const float* C,
                              const float* skip, float* y, int64_t batch, int64_t channels,
                              int64_t L, vmb_stream_t stream) {

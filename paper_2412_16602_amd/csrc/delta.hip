@@ -1,0 +1,155 @@
+// delta.hip -- launches of the chunked gated delta rule, forward and backward.
+#include "delta_kernels.h"
+
+namespace vmb {
+namespace delta {
+namespace {
+
+// Planes of the computed operands (state, errors, T, P): three (binary32's 24
+// bits) for binary32 inputs and where a binary32 output hangs on them, two
+// (16 bits) where every output is bfloat16 (8 bits).
+constexpr int kMostPlanes = 3;
+
+int padded_dk(int64_t dk) { return dk <= 32 ? 32 : dk <= 64 ? 64 : 128; }
+
+struct Layout {
+    size_t KA, QA, KT, QT, TA, PA, TT, gates, S0, dS, E, dR, total;
+    int64_t slots;
+};
+
+Layout layout_of(bool backward, int64_t batch, int64_t L, int64_t n_seq, bool packed,
+                 int64_t heads_k, int64_t heads_v, int64_t dk, int64_t dv, vmb_dtype dt) {
+    const int64_t C = dt == VMB_BF16 ? Planes<bf16_t>::kChunk : Planes<float>::kChunk;
+    const int64_t nx = dt == VMB_BF16 ? 1 : 3;
+    Layout o{};
+    o.slots = packed ? L / C + n_seq : n_seq * ((L + C - 1) / C);
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        const size_t p = at;
+        at += (bytes + 255) & ~size_t{255};
+        return p;
+    };
+    const size_t ks = static_cast<size_t>(o.slots) * heads_k, vs = static_cast<size_t>(o.slots) * heads_v;
+    const size_t key = ks * C * padded_dk(dk) * nx * 2, tri = vs * C * C * kMostPlanes * 2;
+    o.KA = take(key);
+    o.QA = take(key);
+    o.KT = take(key);
+    o.QT = take(backward ? key : 0);
+    o.TA = take(tri);
+    o.PA = take(tri);
+    o.TT = take(backward ? tri : 0);
+    o.gates = take(vs * kGates * C * 4);
+    o.S0 = take(backward ? vs * dk * dv * 4 : 0);
+    o.dS = take(backward ? vs * dk * dv * 4 : 0);
+    o.E = take(backward ? vs * C * dv * 4 : 0);
+    o.dR = take(backward ? vs * C * dv * 4 : 0);
+    o.total = at;
+    return o;
+}
+
+Sizes sizes_of(const DeltaArgs& a, int64_t slots) {
+    Sizes z{};
+    z.cu = a.cu;
+    z.L = a.L, z.tokens = a.batch * a.L, z.n_seq = a.n_seq, z.slots = slots;
+    z.heads_k = static_cast<int>(a.heads_k), z.heads_v = static_cast<int>(a.heads_v);
+    z.group = z.heads_v / z.heads_k;
+    z.dk = static_cast<int>(a.dk), z.dv = static_cast<int>(a.dv);
+    z.q_stride = a.q_stride, z.k_stride = a.k_stride, z.v_stride = a.v_stride;
+    z.scale = a.scale;
+    return z;
+}
+
+Streams streams_of(void* ws, const Layout& o) {
+    char* p = static_cast<char*>(ws);
+    Streams s;
+    s.KA = reinterpret_cast<__bf16*>(p + o.KA);
+    s.QA = reinterpret_cast<__bf16*>(p + o.QA);
+    s.KT = reinterpret_cast<__bf16*>(p + o.KT);
+    s.QT = reinterpret_cast<__bf16*>(p + o.QT);
+    s.TA = reinterpret_cast<__bf16*>(p + o.TA);
+    s.PA = reinterpret_cast<__bf16*>(p + o.PA);
+    s.TT = reinterpret_cast<__bf16*>(p + o.TT);
+    s.gates = reinterpret_cast<float*>(p + o.gates);
+    s.S0 = reinterpret_cast<float*>(p + o.S0);
+    s.dS = reinterpret_cast<float*>(p + o.dS);
+    s.E = reinterpret_cast<float*>(p + o.E);
+    s.dR = reinterpret_cast<float*>(p + o.dR);
+    return s;
+}
+
+template <typename In, int NS, int DK>
+void forward(const DeltaArgs& a, const Sizes& z, const Streams& ws) {
+    constexpr int C = Planes<In>::kChunk;
+    const dim3 chunks(static_cast<unsigned>(z.slots), static_cast<unsigned>(z.heads_v));
+    k_delta_prepare<In, NS, DK, false>
+        <<<chunks, C * 4, 0, a.stream>>>(z, a.q, a.k, a.g, a.beta, ws);
+    const dim3 columns(static_cast<unsigned>(z.n_seq), static_cast<unsigned>(z.heads_v),
+                       static_cast<unsigned>((z.dv + 15) / 16));
+    k_delta_walk<In, NS, DK, true, false>
+        <<<columns, 64, 0, a.stream>>>(z, a.v, a.h0, a.o, a.hT, ws);
+}
+
+template <typename In, int NS, int DK>
+void backward(const DeltaArgs& a, const Sizes& z, const Streams& ws) {
+    constexpr int C = Planes<In>::kChunk;
+    const dim3 chunks(static_cast<unsigned>(z.slots), static_cast<unsigned>(z.heads_v));
+    k_delta_prepare<In, NS, DK, true>
+        <<<chunks, C * 4, 0, a.stream>>>(z, a.q, a.k, a.g, a.beta, ws);
+    const dim3 columns(static_cast<unsigned>(z.n_seq), static_cast<unsigned>(z.heads_v),
+                       static_cast<unsigned>((z.dv + 15) / 16));
+    k_delta_walk<In, NS, DK, false, true>
+        <<<columns, 64, 0, a.stream>>>(z, a.v, a.h0, nullptr, nullptr, ws);
+    k_delta_walk_back<In, NS, DK>
+        <<<columns, 64, 0, a.stream>>>(z, a.d_o, a.d_hT, a.d_v, a.d_h0, ws);
+    const dim3 keys(static_cast<unsigned>(z.slots), static_cast<unsigned>(z.heads_k));
+    k_delta_grads<In, NS, DK><<<keys, C * 4, 0, a.stream>>>(z, a.q, a.k, a.d_o, a.d_q, a.d_k, a.g,
+                                                            a.h0 == nullptr, a.d_g, a.d_beta, ws);
+}
+
+template <typename In, int NS>
+void by_width(const DeltaArgs& a, const Sizes& z, const Streams& ws, bool back) {
+    switch (padded_dk(a.dk)) {
+        case 32: back ? backward<In, NS, 32>(a, z, ws) : forward<In, NS, 32>(a, z, ws); break;
+        case 64: back ? backward<In, NS, 64>(a, z, ws) : forward<In, NS, 64>(a, z, ws); break;
+        default: back ? backward<In, NS, 128>(a, z, ws) : forward<In, NS, 128>(a, z, ws);
+    }
+}
+
+vmb_status launch(const DeltaArgs& a, bool back) {
+    const Layout o = layout_of(back, a.batch, a.L, a.n_seq, a.cu != nullptr, a.heads_k, a.heads_v,
+                               a.dk, a.dv, a.dt);
+    // a grid's first dimension holds 2^32 threads
+    if (o.slots > (int64_t{1} << 23) || a.n_seq > (int64_t{1} << 23)) return VMB_ERR_UNSUPPORTED;
+    const Sizes z = sizes_of(a, o.slots);
+    const Streams ws = streams_of(a.ws, o);
+    if (a.dt == VMB_F32) by_width<float, 3>(a, z, ws, back);
+    else if (back || a.hT) by_width<bf16_t, 3>(a, z, ws, back);
+    else by_width<bf16_t, 2>(a, z, ws, back);
+    return check_launch();
+}
+
+}  // namespace
+}  // namespace delta
+
+size_t delta_workspace_bytes(bool backward, int64_t batch, int64_t L, int64_t n_seq,
+                             int64_t heads_k, int64_t heads_v, int64_t dk, int64_t dv,
+                             vmb_dtype dt) {
+    constexpr int64_t kMost = int64_t{1} << 40;
+    if (batch < 1 || L < 1 || n_seq < 1 || heads_k < 1 || heads_v < 1 || dk < 1 || dv < 1 ||
+        dk > 128 || dv > 256 || heads_v > 65535 || heads_k > heads_v ||
+        (dt != VMB_F32 && dt != VMB_BF16) || batch > kMost / L ||
+        batch * L > kMost / heads_v || n_seq > kMost / heads_v)
+        return SIZE_MAX;
+    // packed sequences have batch 1; n_seq == batch may be either
+    const size_t rows =
+        delta::layout_of(backward, batch, L, n_seq, false, heads_k, heads_v, dk, dv, dt).total;
+    if (batch != 1) return rows;
+    const size_t packed =
+        delta::layout_of(backward, batch, L, n_seq, true, heads_k, heads_v, dk, dv, dt).total;
+    return n_seq > 1 ? packed : (packed > rows ? packed : rows);
+}
+
+vmb_status launch_delta_fwd(const DeltaArgs& a) { return delta::launch(a, false); }
+vmb_status launch_delta_bwd(const DeltaArgs& a) { return delta::launch(a, true); }
+
+}  // namespace vmb

@@ -1,0 +1,271 @@
+// rotary.hip -- rotary positions with several axes, forward and backward, with
+// the optional L2 norm of each head.
+//
+// Pair j of a head turns by theta = position[axis(j)] * inv_freq[j]. A
+// workgroup takes a run of tokens: it forms the cosines and sines of its
+// (token, pair) angles once, in LDS, and its threads then pass over the
+// tokens' heads (both tensors), lanes_per_head lanes to a head, each holding
+// the two vectors of V elements that V pairs need. The angle is formed and
+// reduced to one turn in binary64 (exact products: 31-bit positions of
+// 24-bit frequencies), because in binary32 a position of 10^4 would already
+// cost 10^-3 of a radian.
+//
+// Bound by HBM: each element is read and written once (twice read backward
+// with the norm); the sums of the norm are shuffles within a head's lanes.
+#include "vmb_internal.h"
+
+namespace vmb {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kTableMax = 2048;  // (token, pair) angles of a workgroup in LDS
+
+struct RotaryDev {
+    const void *xq, *xk, *inq, *ink;
+    void *yq, *yk;
+    const int32_t* positions;
+    const float* inv_freq;
+    int64_t tokens, L, runs;       // batch * L, L, runs of tile tokens
+    int64_t q_stride, k_stride;    // strides of the strided side
+    int64_t pos_batch_stride;      // 0 when the positions are shared
+    int heads_q, heads, dim, pairs, items, lanes_log2, tile;
+    int n_axes;
+    int section_end[kRotaryMaxAxes];
+    int interleaved;
+    float eps;
+};
+
+template <typename T, int V>
+struct alignas(sizeof(T) * V) Vec {
+    T v[V];
+};
+
+template <typename T, int V>
+__device__ __forceinline__ void load(const T* p, float (&f)[V]) {
+    const Vec<T, V> x = *reinterpret_cast<const Vec<T, V>*>(p);
+#pragma unroll
+    for (int i = 0; i < V; ++i) f[i] = to_f32(x.v[i]);
+}
+template <typename T, int V>
+__device__ __forceinline__ void store(T* p, const float (&f)[V]) {
+    Vec<T, V> x;
+#pragma unroll
+    for (int i = 0; i < V; ++i) x.v[i] = from_f32<T>(f[i]);
+    *reinterpret_cast<Vec<T, V>*>(p) = x;
+}
+
+template <typename T, int V, bool kNorm, bool kBack>
+__global__ __launch_bounds__(kThreads) void k_rotary(const RotaryDev a) {
+    __shared__ float2 table[kTableMax];
+  for (int64_t run = blockIdx.x; run < a.runs; run += gridDim.x) {
+    const int64_t t0 = run * a.tile;
+    const int n_tok = static_cast<int>(a.tokens - t0 < a.tile ? a.tokens - t0 : a.tile);
+    for (int e = threadIdx.x; e < n_tok * a.pairs; e += kThreads) {
+        const int tok = e / a.pairs, j = e - tok * a.pairs;
+        const int64_t t = t0 + tok, b = t / a.L;
+        int axis = 0;
+        while (axis < a.n_axes - 1 && j >= a.section_end[axis]) ++axis;
+        const int32_t pos =
+            a.positions[b * a.pos_batch_stride + (t - b * a.L) * a.n_axes + axis];
+        constexpr double kTurn = 6.283185307179586476925;
+        const double angle = static_cast<double>(pos) * static_cast<double>(a.inv_freq[j]);
+        const double turns = rint(angle * (1.0 / kTurn));
+        float s, c;
+        sincosf(static_cast<float>(__builtin_fma(-turns, kTurn, angle)), &s, &c);
+        table[e] = make_float2(c, kBack ? -s : s);
+    }
+    __syncthreads();
+
+    const int lanes = 1 << a.lanes_log2;
+    const int lane = threadIdx.x & (lanes - 1);
+    const int pair_items = a.pairs / V;
+    const int tasks = n_tok * a.heads;
+    for (int task = threadIdx.x >> a.lanes_log2; task < tasks;
+         task += kThreads >> a.lanes_log2) {
+        const int tok = task / a.heads, h = task - tok * a.heads;
+        const bool first = h < a.heads_q;
+        const int hh = first ? h : h - a.heads_q;
+        const int64_t t = t0 + tok;
+        const int64_t flat = t * ((first ? a.heads_q : a.heads - a.heads_q)) + hh;
+        const int64_t at_strided =
+            t * (first ? a.q_stride : a.k_stride) + static_cast<int64_t>(hh) * a.dim;
+        const int64_t at = flat * a.dim;
+        const T* x = static_cast<const T*>(first ? a.xq : a.xk) + (kBack ? at : at_strided);
+        const T* in = static_cast<const T*>(first ? a.inq : a.ink) + at_strided;
+        T* y = static_cast<T*>(first ? a.yq : a.yk) + at;
+        const float2* cs = table + tok * a.pairs;
+
+        // offsets of an item's two vectors (the second is absent past the pairs)
+        auto place = [&](int item, int& o1, int& o2) {
+            if (item < pair_items) {
+                o1 = a.interleaved ? 2 * V * item : V * item;
+                o2 = a.interleaved ? o1 + V : a.pairs + V * item;
+                return true;
+            }
+            o1 = 2 * a.pairs + V * (item - pair_items);
+            o2 = o1;
+            return false;
+        };
+        // turns the item's pairs in place
+        auto turn = [&](int item, float (&u)[V], float (&w)[V]) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float2 c = cs[V * item + i];
+                if (a.interleaved && V > 1) {
+                    // pairs lie side by side: (u0, u1), (u2, u3), .. then w
+                    constexpr int kHalf = V > 1 ? V / 2 : 1;
+                    float(&s)[V] = i < kHalf ? u : w;
+                    const int k = 2 * (i % kHalf);
+                    const float p = s[k], q = s[(k + 1) % V];
+                    s[k] = p * c.x - q * c.y;
+                    s[(k + 1) % V] = p * c.y + q * c.x;
+                } else {
+                    const float p = u[i], q = w[i];
+                    u[i] = p * c.x - q * c.y;
+                    w[i] = p * c.y + q * c.x;
+                }
+            }
+        };
+
+        float u[V], w[V], xu[V], xw[V];
+        float sq = 0.0f, dot = 0.0f;
+        // the item's values, turned (backward: turned gradients, and the
+        // inputs in xu, xw); adds to the sums
+        auto fetch = [&](int item) {
+            int o1, o2;
+            const bool pair = place(item, o1, o2);
+            load<T, V>(x + o1, u);
+            if (pair) load<T, V>(x + o2, w);
+            if constexpr (kNorm && kBack) {
+                load<T, V>(in + o1, xu);
+                if (pair) load<T, V>(in + o2, xw);
+            }
+            if (pair) turn(item, u, w);
+            if constexpr (kNorm) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    // a rotation keeps the length, so the forward sums the
+                    // turned values
+                    const float p = kBack ? xu[i] : u[i];
+                    sq = __builtin_fmaf(p, p, sq);
+                    if (kBack) dot = __builtin_fmaf(p, u[i], dot);
+                    if (pair) {
+                        const float q = kBack ? xw[i] : w[i];
+                        sq = __builtin_fmaf(q, q, sq);
+                        if (kBack) dot = __builtin_fmaf(q, w[i], dot);
+                    }
+                }
+            }
+        };
+        auto put = [&](int item, float r, float m) {
+            int o1, o2;
+            const bool pair = place(item, o1, o2);
+            if constexpr (kNorm) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    u[i] = kBack ? r * (u[i] - xu[i] * m) : r * u[i];
+                    if (pair) w[i] = kBack ? r * (w[i] - xw[i] * m) : r * w[i];
+                }
+            }
+            store<T, V>(y + o1, u);
+            if (pair) store<T, V>(y + o2, w);
+        };
+
+        if (lane < a.items) fetch(lane);
+        float r = 1.0f, m = 0.0f;
+        if constexpr (kNorm) {
+            for (int item = lane + lanes; item < a.items; item += lanes) fetch(item);
+            for (int k = lanes / 2; k > 0; k /= 2) {
+                sq += __shfl_xor(sq, k);
+                if (kBack) dot += __shfl_xor(dot, k);
+            }
+            r = 1.0f / sqrtf(sq + a.eps);
+            m = dot * r * r;
+        }
+        // heads of more items than lanes: the others are fetched again
+        if (a.items > lanes) {
+            for (int item = lane; item < a.items; item += lanes) {
+                fetch(item);
+                put(item, r, m);
+            }
+        } else if (lane < a.items) {
+            put(lane, r, m);
+        }
+    }
+    __syncthreads();  // the table is written again
+  }
+}
+
+template <typename T, int V>
+void launch_v(const RotaryDev& d, bool norm, bool back, hipStream_t s) {
+    constexpr int64_t kMostGroups = 1 << 22;  // a grid holds 2^32 threads; further runs follow
+    const dim3 grid(static_cast<unsigned>(d.runs < kMostGroups ? d.runs : kMostGroups));
+    if (back) {
+        if (norm)
+            k_rotary<T, V, true, true><<<grid, kThreads, 0, s>>>(d);
+        else
+            k_rotary<T, V, false, true><<<grid, kThreads, 0, s>>>(d);
+    } else if (norm) {
+        k_rotary<T, V, true, false><<<grid, kThreads, 0, s>>>(d);
+    } else {
+        k_rotary<T, V, false, false><<<grid, kThreads, 0, s>>>(d);
+    }
+}
+
+}  // namespace
+
+vmb_status launch_rotary(const RotaryArgs& a, bool backward) {
+    RotaryDev d{};
+    const bool norm = (a.options & VMB_ROTARY_NORM) != 0;
+    const bool strides = !backward || norm;
+    const int64_t heads_k = a.xk ? a.heads_k : 0;
+    d.xq = a.xq, d.xk = a.xk, d.inq = a.inq, d.ink = a.ink, d.yq = a.yq, d.yk = a.yk;
+    d.positions = a.positions, d.inv_freq = a.inv_freq;
+    d.tokens = a.batch * a.L, d.L = a.L;
+    d.q_stride = strides ? a.q_stride : a.heads_q * a.dim;
+    d.k_stride = strides ? a.k_stride : heads_k * a.dim;
+    d.pos_batch_stride = a.positions_batch > 1 ? a.L * a.n_axes : 0;
+    d.heads_q = static_cast<int>(a.heads_q);
+    d.heads = static_cast<int>(a.heads_q + heads_k);
+    d.dim = static_cast<int>(a.dim);
+    d.n_axes = static_cast<int>(a.n_axes);
+    for (int i = 0; i < d.n_axes; ++i) {
+        d.pairs += static_cast<int>(a.sections[i]);
+        d.section_end[i] = d.pairs;
+    }
+    d.interleaved = (a.options & VMB_ROTARY_INTERLEAVED) != 0;
+    d.eps = a.eps;
+    // the widest vector (16 bytes at most) that divides every offset
+    const int e = a.dt == VMB_BF16 ? 2 : 4;
+    int v = 16 / e;
+    auto fits = [&](int n) {
+        if (d.pairs % n || d.dim % n) return false;
+        if (strides && (a.q_stride % n || (a.xk && a.k_stride % n))) return false;
+        for (const void* p : {d.xq, d.xk, d.inq, d.ink, static_cast<const void*>(d.yq),
+                              static_cast<const void*>(d.yk)})
+            if (reinterpret_cast<uintptr_t>(p) % (n * e)) return false;
+        return true;
+    };
+    while (v > 1 && !fits(v)) v /= 2;
+    d.items = d.pairs / v + (d.dim - 2 * d.pairs) / v;
+    while ((1 << d.lanes_log2) < d.items && d.lanes_log2 < 6) ++d.lanes_log2;
+    // tokens of a workgroup: enough workgroups for the chip first, then
+    // enough work to pay for the angles
+    int64_t tile = (d.tokens + 2047) / 2048;
+    const int64_t most = kTableMax / d.pairs < 16 ? kTableMax / d.pairs : 16;
+    d.tile = static_cast<int>(tile > most ? most : tile);
+    d.runs = (d.tokens + d.tile - 1) / d.tile;
+    if (a.dt == VMB_BF16) {
+        if (v == 8) launch_v<bf16_t, 8>(d, norm, backward, a.stream);
+        else if (v == 4) launch_v<bf16_t, 4>(d, norm, backward, a.stream);
+        else if (v == 2) launch_v<bf16_t, 2>(d, norm, backward, a.stream);
+        else launch_v<bf16_t, 1>(d, norm, backward, a.stream);
+    } else {
+        if (v == 4) launch_v<float, 4>(d, norm, backward, a.stream);
+        else if (v == 2) launch_v<float, 2>(d, norm, backward, a.stream);
+        else launch_v<float, 1>(d, norm, backward, a.stream);
+    }
+    return check_launch();
+}
+
+}  // namespace vmb

@@ -1,0 +1,229 @@
+// validate_mixer.cpp -- host-side argument checks of the gated delta rule, the
+// rotary positions and the channels-last group norm. Pure C++: no HIP calls.
+#include <stdint.h>
+
+#include <cmath>
+#include <initializer_list>
+
+#include "vmb_internal.h"
+
+namespace vmb {
+namespace {
+
+constexpr int64_t kMaxRow = (int64_t{1} << 31) - 1;
+constexpr int64_t kMaxTotal = int64_t{1} << 40;
+
+bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+bool valid_dtype(vmb_dtype t) { return t == VMB_F32 || t == VMB_BF16; }
+int64_t dsize(vmb_dtype t) { return t == VMB_BF16 ? 2 : 4; }
+
+// overflow-checked product of positive sizes; -1 past kMaxTotal
+int64_t prod(std::initializer_list<int64_t> v) {
+    int64_t r = 1;
+    for (int64_t x : v) {
+        if (x <= 0 || r > kMaxTotal / x) return -1;
+        r *= x;
+    }
+    return r;
+}
+
+struct Buffer {
+    const void* p;
+    int64_t bytes;
+};
+
+bool overlap(const Buffer& a, const Buffer& b) {
+    if (!a.p || !b.p) return false;
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+    return x < y + static_cast<uintptr_t>(b.bytes) && y < x + static_cast<uintptr_t>(a.bytes);
+}
+
+// No output may touch an input or another output.
+bool aliased(std::initializer_list<Buffer> in, std::initializer_list<Buffer> out) {
+    for (auto o = out.begin(); o != out.end(); ++o) {
+        for (const Buffer& i : in)
+            if (overlap(*o, i)) return true;
+        for (auto p = o + 1; p != out.end(); ++p)
+            if (overlap(*o, *p)) return true;
+    }
+    return false;
+}
+
+// Elements from the first to the last of a [batch, L, heads, d] tensor whose
+// tokens are stride apart; -1 for sizes or a stride that do not fit.
+int64_t strided(int64_t batch, int64_t L, int64_t heads, int64_t d, int64_t stride) {
+    const int64_t row = prod({heads, d});
+    if (row < 0 || stride < row || row > kMaxRow) return -1;
+    const int64_t all = prod({batch, L, stride});
+    return all < 0 ? -1 : all - stride + row;
+}
+
+vmb_status delta_sizes(int64_t batch, int64_t L, int64_t heads_k, int64_t heads_v, int64_t dk,
+                       int64_t dv) {
+    if (batch < 1 || L < 1 || heads_k < 1 || heads_v < 1 || dk < 1 || dv < 1) return VMB_ERR_SHAPE;
+    if (L > kMaxRow || heads_v % heads_k != 0 || heads_v > 65535) return VMB_ERR_SHAPE;
+    if (prod({batch, L, heads_v}) < 0 || prod({batch, heads_v, dk, dv}) < 0) return VMB_ERR_SHAPE;
+    if (dk % 8 != 0 || dv % 8 != 0 || dk > 128 || dv > 256) return VMB_ERR_UNSUPPORTED;
+    return VMB_OK;
+}
+
+}  // namespace
+
+vmb_status validate_delta(const DeltaArgs& a, bool backward) {
+    if (!a.q || !a.k || !a.v || !a.g || !a.beta) return VMB_ERR_NULL;
+    if (backward ? !a.d_o || !a.d_q || !a.d_k || !a.d_v || !a.d_g || !a.d_beta : !a.o)
+        return VMB_ERR_NULL;
+    if (!valid_dtype(a.dt)) return VMB_ERR_DTYPE;
+    const vmb_status st = delta_sizes(a.batch, a.L, a.heads_k, a.heads_v, a.dk, a.dv);
+    if (st != VMB_OK) return st;
+    if (!std::isfinite(a.scale) || a.n_seq < 1 || a.n_seq > kMaxRow) return VMB_ERR_SHAPE;
+    if (a.cu ? a.batch != 1 : a.n_seq != a.batch) return VMB_ERR_SHAPE;
+    const int64_t e = dsize(a.dt);
+    const int64_t nq = strided(a.batch, a.L, a.heads_k, a.dk, a.q_stride);
+    const int64_t nk = strided(a.batch, a.L, a.heads_k, a.dk, a.k_stride);
+    const int64_t nv = strided(a.batch, a.L, a.heads_v, a.dv, a.v_stride);
+    const int64_t no = prod({a.batch, a.L, a.heads_v, a.dv});
+    const int64_t nqo = prod({a.batch, a.L, a.heads_k, a.dk});
+    const int64_t ns = prod({a.n_seq, a.heads_v, a.dk, a.dv});
+    const int64_t ng = prod({a.batch, a.L, a.heads_v});
+    if (nq < 0 || nk < 0 || nv < 0 || no < 0 || nqo < 0 || ns < 0 || ng < 0) return VMB_ERR_SHAPE;
+    if (a.q_stride * e % 16 || a.k_stride * e % 16 || a.v_stride * e % 16) return VMB_ERR_SHAPE;
+    for (const void* p : {a.q, a.k, a.v, static_cast<const void*>(a.o), a.d_o,
+                          static_cast<const void*>(a.d_q), static_cast<const void*>(a.d_k),
+                          static_cast<const void*>(a.d_v), static_cast<const void*>(a.h0),
+                          static_cast<const void*>(a.hT), static_cast<const void*>(a.d_hT),
+                          static_cast<const void*>(a.d_h0), static_cast<const void*>(a.ws)})
+        if (!aligned(p, 16)) return VMB_ERR_ALIGN;
+    for (const void* p : {static_cast<const void*>(a.g), static_cast<const void*>(a.beta),
+                          static_cast<const void*>(a.cu), static_cast<const void*>(a.d_g),
+                          static_cast<const void*>(a.d_beta)})
+        if (!aligned(p, 4)) return VMB_ERR_ALIGN;
+    const size_t need = delta_workspace_bytes(backward, a.batch, a.L, a.n_seq, a.heads_k,
+                                              a.heads_v, a.dk, a.dv, a.dt);
+    if (need == SIZE_MAX) return VMB_ERR_SHAPE;
+    if (need > 0 && (!a.ws || a.ws_bytes < need)) return VMB_ERR_WORKSPACE;
+    const Buffer ws{need ? a.ws : nullptr, static_cast<int64_t>(need)};
+    const int64_t cu = (a.n_seq + 1) * 4;
+    if (backward
+            ? aliased({{a.q, nq * e}, {a.k, nk * e}, {a.v, nv * e}, {a.g, ng * 4},
+                       {a.beta, ng * 4}, {a.h0, ns * 4}, {a.cu, cu}, {a.d_o, no * e},
+                       {a.d_hT, ns * 4}},
+                      {{a.d_q, nqo * e}, {a.d_k, nqo * e}, {a.d_v, no * e}, {a.d_g, ng * 4},
+                       {a.d_beta, ng * 4}, {a.d_h0, ns * 4}, ws})
+            : aliased({{a.q, nq * e}, {a.k, nk * e}, {a.v, nv * e}, {a.g, ng * 4},
+                       {a.beta, ng * 4}, {a.h0, ns * 4}, {a.cu, cu}},
+                      {{a.o, no * e}, {a.hT, ns * 4}, ws}))
+        return VMB_ERR_ALIAS;
+    return VMB_OK;
+}
+
+vmb_status validate_delta_step(const DeltaStepArgs& a) {
+    if (!a.q || !a.k || !a.v || !a.g || !a.beta || !a.state || !a.o) return VMB_ERR_NULL;
+    if (!valid_dtype(a.dt)) return VMB_ERR_DTYPE;
+    const vmb_status st = delta_sizes(a.batch, a.T, a.heads_k, a.heads_v, a.dk, a.dv);
+    if (st != VMB_OK) return st;
+    if (!std::isfinite(a.scale) || a.n_slots < 1 || a.n_slots > kMaxRow || a.batch > kMaxRow)
+        return VMB_ERR_SHAPE;
+    if (!a.slots && a.n_slots < a.batch) return VMB_ERR_SHAPE;
+    const int64_t e = dsize(a.dt);
+    const int64_t nq = strided(a.batch, a.T, a.heads_k, a.dk, a.q_stride);
+    const int64_t nk = strided(a.batch, a.T, a.heads_k, a.dk, a.k_stride);
+    const int64_t nv = strided(a.batch, a.T, a.heads_v, a.dv, a.v_stride);
+    const int64_t no = prod({a.batch, a.T, a.heads_v, a.dv});
+    const int64_t ns = prod({a.n_slots, a.heads_v, a.dk, a.dv});
+    const int64_t ng = prod({a.batch, a.T, a.heads_v});
+    if (nq < 0 || nk < 0 || nv < 0 || no < 0 || ns < 0 || ng < 0) return VMB_ERR_SHAPE;
+    if (a.q_stride * e % 16 || a.k_stride * e % 16 || a.v_stride * e % 16) return VMB_ERR_SHAPE;
+    for (const void* p : {a.q, a.k, a.v, static_cast<const void*>(a.o),
+                          static_cast<const void*>(a.state)})
+        if (!aligned(p, 16)) return VMB_ERR_ALIGN;
+    if (!aligned(a.g, 4) || !aligned(a.beta, 4) || !aligned(a.slots, 4)) return VMB_ERR_ALIGN;
+    if (aliased({{a.q, nq * e}, {a.k, nk * e}, {a.v, nv * e}, {a.g, ng * 4}, {a.beta, ng * 4},
+                 {a.slots, a.batch * 4}},
+                {{a.o, no * e}, {a.state, ns * 4}}))
+        return VMB_ERR_ALIAS;
+    return VMB_OK;
+}
+
+vmb_status validate_rotary(const RotaryArgs& a, bool backward) {
+    const bool norm = (a.options & VMB_ROTARY_NORM) != 0;
+    if (!a.xq || !a.yq || !a.positions || !a.inv_freq || !a.sections) return VMB_ERR_NULL;
+    if ((a.xk == nullptr) != (a.yk == nullptr)) return VMB_ERR_NULL;
+    if (backward && norm && (!a.inq || (a.xk && !a.ink))) return VMB_ERR_NULL;
+    if (!valid_dtype(a.dt)) return VMB_ERR_DTYPE;
+    const int64_t hk = a.xk ? a.heads_k : 1;
+    if (a.batch < 1 || a.L < 1 || a.heads_q < 1 || hk < 1 || a.dim < 1 || a.n_axes < 1 ||
+        a.L > kMaxRow || a.heads_q > 65535 || hk > 65535)
+        return VMB_ERR_SHAPE;
+    if ((a.options & ~static_cast<unsigned>(VMB_ROTARY_INTERLEAVED | VMB_ROTARY_NORM)) != 0)
+        return VMB_ERR_UNSUPPORTED;
+    if (a.dim % 2 != 0 || a.dim > 512 || a.n_axes > kRotaryMaxAxes) return VMB_ERR_UNSUPPORTED;
+    if (a.positions_batch != 1 && a.positions_batch != a.batch) return VMB_ERR_SHAPE;
+    int64_t pairs = 0;
+    for (int64_t i = 0; i < a.n_axes; ++i) {
+        if (a.sections[i] < 0 || a.sections[i] > a.dim) return VMB_ERR_SHAPE;
+        pairs += a.sections[i];
+    }
+    if (pairs < 1 || pairs > a.dim / 2) return VMB_ERR_SHAPE;
+    if (norm && !(a.eps >= 0.0f && std::isfinite(a.eps))) return VMB_ERR_SHAPE;
+    const int64_t e = dsize(a.dt);
+    const int64_t np = prod({a.positions_batch, a.L, a.n_axes});
+    const int64_t nyq = prod({a.batch, a.L, a.heads_q, a.dim});
+    const int64_t nyk = prod({a.batch, a.L, hk, a.dim});
+    if (np < 0 || nyq < 0 || nyk < 0) return VMB_ERR_SHAPE;
+    // forward reads q and k by their strides; backward only with the norm
+    const bool strides = !backward || norm;
+    const int64_t nq = strides ? strided(a.batch, a.L, a.heads_q, a.dim, a.q_stride) : nyq;
+    const int64_t nk = strides && a.xk ? strided(a.batch, a.L, hk, a.dim, a.k_stride) : nyk;
+    if (nq < 0 || nk < 0) return VMB_ERR_SHAPE;
+    for (const void* p : {a.xq, a.xk, a.inq, a.ink, static_cast<const void*>(a.yq),
+                          static_cast<const void*>(a.yk)})
+        if (!aligned(p, static_cast<uintptr_t>(e))) return VMB_ERR_ALIGN;
+    if (!aligned(a.positions, 4) || !aligned(a.inv_freq, 4)) return VMB_ERR_ALIGN;
+    const void* inq = backward && norm ? a.inq : nullptr;
+    const void* ink = backward && norm && a.xk ? a.ink : nullptr;
+    if (aliased({{a.xq, (backward ? nyq : nq) * e}, {a.xk, (backward ? nyk : nk) * e},
+                 {inq, nq * e}, {ink, nk * e}, {a.positions, np * 4}, {a.inv_freq, pairs * 4}},
+                {{a.yq, nyq * e}, {a.yk, nyk * e}}))
+        return VMB_ERR_ALIAS;
+    return VMB_OK;
+}
+
+vmb_status validate_group_norm(const GroupNormArgs& a, bool backward) {
+    if (!a.x || !a.out) return VMB_ERR_NULL;
+    if (backward && (!a.dy || !a.mean || !a.rstd)) return VMB_ERR_NULL;
+    if ((a.mean == nullptr) != (a.rstd == nullptr) ||
+        (a.dgamma == nullptr) != (a.dbeta == nullptr))
+        return VMB_ERR_NULL;
+    if (!valid_dtype(a.dt)) return VMB_ERR_DTYPE;
+    if (a.batch < 1 || a.P < 1 || a.channels < 1 || a.groups < 1 || a.batch > 65535 ||
+        a.channels % a.groups != 0 || prod({a.P, a.channels}) > kMaxRow ||
+        prod({a.P, a.channels}) < 0)
+        return VMB_ERR_SHAPE;
+    if (!backward && !(a.eps >= 0.0f && std::isfinite(a.eps))) return VMB_ERR_SHAPE;
+    if ((a.act != VMB_ACT_NONE && a.act != VMB_ACT_SILU) || a.channels > 16384)
+        return VMB_ERR_UNSUPPORTED;
+    const int64_t n = prod({a.batch, a.P, a.channels}), e = dsize(a.dt);
+    if (n < 0) return VMB_ERR_SHAPE;
+    for (const void* p : {a.x, a.dy, static_cast<const void*>(a.out),
+                          static_cast<const void*>(a.ws)})
+        if (!aligned(p, 16)) return VMB_ERR_ALIGN;
+    for (const float* p : {a.gamma, a.beta, static_cast<const float*>(a.mean),
+                           static_cast<const float*>(a.rstd), static_cast<const float*>(a.dgamma),
+                           static_cast<const float*>(a.dbeta)})
+        if (!aligned(p, 4)) return VMB_ERR_ALIGN;
+    const size_t need =
+        group_norm_workspace_bytes(backward, a.batch, a.P, a.channels, a.groups);
+    if (need > 0 && (!a.ws || a.ws_bytes < need)) return VMB_ERR_WORKSPACE;
+    const Buffer ws{need ? a.ws : nullptr, static_cast<int64_t>(need)};
+    const int64_t c = a.channels * 4, s = a.batch * a.groups * 4;
+    if (backward ? aliased({{a.x, n * e}, {a.dy, n * e}, {a.gamma, c}, {a.beta, c}, {a.mean, s},
+                            {a.rstd, s}},
+                           {{a.out, n * e}, {a.dgamma, c}, {a.dbeta, c}, ws})
+                 : aliased({{a.x, n * e}, {a.gamma, c}, {a.beta, c}},
+                           {{a.out, n * e}, {a.mean, s}, {a.rstd, s}, ws}))
+        return VMB_ERR_ALIAS;
+    return VMB_OK;
+}
+
+}  // namespace vmb

@@ -51,6 +51,85 @@ vmb_status validate_projections(const void* u, const float* W, const float* W_dt
                                 int64_t K, int64_t channels, int64_t L, int64_t N, int64_t R,
                                 vmb_dtype dt);
 
+// Gated delta rule, forward (o, hT) and backward (the gradients) alike.
+struct DeltaArgs {
+    const void *q, *k, *v;
+    const float *g, *beta, *h0;
+    const int32_t* cu;
+    void* o;
+    float* hT;
+    const void* d_o;
+    const float* d_hT;
+    void *d_q, *d_k, *d_v;
+    float *d_g, *d_beta, *d_h0;
+    int64_t batch, L, n_seq, heads_k, heads_v, dk, dv;
+    int64_t q_stride, k_stride, v_stride;
+    float scale;
+    vmb_dtype dt;
+    void* ws;
+    size_t ws_bytes;
+    hipStream_t stream;
+};
+struct DeltaStepArgs {
+    const void *q, *k, *v;
+    const float *g, *beta;
+    const int32_t* slots;
+    float* state;
+    void* o;
+    int64_t batch, T, n_slots, heads_k, heads_v, dk, dv;
+    int64_t q_stride, k_stride, v_stride;
+    float scale;
+    vmb_dtype dt;
+    hipStream_t stream;
+};
+vmb_status validate_delta(const DeltaArgs& a, bool backward);
+vmb_status validate_delta_step(const DeltaStepArgs& a);
+size_t delta_workspace_bytes(bool backward, int64_t batch, int64_t L, int64_t n_seq,
+                             int64_t heads_k, int64_t heads_v, int64_t dk, int64_t dv,
+                             vmb_dtype dt);
+vmb_status launch_delta_fwd(const DeltaArgs& a);
+vmb_status launch_delta_bwd(const DeltaArgs& a);
+vmb_status launch_delta_step(const DeltaStepArgs& a);
+
+// Rotary positions: x* the tensors that are turned (q, k forward; their
+// outputs' gradients backward), in* the forward inputs (backward with the
+// norm only).
+constexpr int kRotaryMaxAxes = 4;
+struct RotaryArgs {
+    const void *xq, *xk, *inq, *ink;
+    const int32_t* positions;
+    const float* inv_freq;
+    const int64_t* sections;
+    void *yq, *yk;
+    int64_t batch, L, heads_q, heads_k, dim, n_axes, positions_batch;
+    int64_t q_stride, k_stride;  // of q and k (forward: xq, xk; backward: inq, ink)
+    unsigned options;
+    float eps;
+    vmb_dtype dt;
+    hipStream_t stream;
+};
+vmb_status validate_rotary(const RotaryArgs& a, bool backward);
+vmb_status launch_rotary(const RotaryArgs& a, bool backward);
+
+struct GroupNormArgs {
+    const void *x, *dy;
+    const float *gamma, *beta;
+    void* out;  // y or dx
+    float *mean, *rstd;  // outputs forward, inputs backward
+    float *dgamma, *dbeta;
+    int64_t batch, P, channels, groups;
+    float eps;
+    vmb_act act;
+    vmb_dtype dt;
+    void* ws;
+    size_t ws_bytes;
+    hipStream_t stream;
+};
+vmb_status validate_group_norm(const GroupNormArgs& a, bool backward);
+size_t group_norm_workspace_bytes(bool backward, int64_t batch, int64_t P, int64_t channels,
+                                  int64_t groups);
+vmb_status launch_group_norm(const GroupNormArgs& a, bool backward);
+
 // Chunk length (positions) of the mean variant's reduce / carry / finish passes.
 constexpr int kMeanChunk = 64;
 

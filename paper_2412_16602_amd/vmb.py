@@ -28,6 +28,9 @@ VMB_MEAN_SKIP_PER_CHANNEL, VMB_MEAN_RAW, VMB_MEAN_NO_BROADCAST, VMB_MEAN_POOLED 
 VMB_MEAN_TEST_GIVE_UP = 1 << 30
 # vmb_scan_option bits (vmb_selective_scan_fwd_ex; vmb_mean_scan_fwd_ex takes them too)
 VMB_SCAN_ZOH = 16
+# vmb_rotary_option bits and vmb_act values
+VMB_ROTARY_INTERLEAVED, VMB_ROTARY_NORM = 1, 2
+VMB_ACT_NONE, VMB_ACT_SILU = 0, 1
 
 STATUS = {0: "VMB_OK", 1: "VMB_ERR_NULL", 2: "VMB_ERR_SHAPE", 3: "VMB_ERR_DTYPE",
           4: "VMB_ERR_ALIGN", 5: "VMB_ERR_ALIAS", 6: "VMB_ERR_UNSUPPORTED",
@@ -82,6 +85,22 @@ def load_library():
     lib.vmb_mean_scan_fwd_noalloc.restype = I
     lib.vmb_mean_scan_status.argtypes = [P, P]
     lib.vmb_mean_scan_status.restype = I
+    F, U, Z = ctypes.c_float, ctypes.c_uint, ctypes.c_size_t
+    lib.vmb_gated_delta_fwd.argtypes = [P] * 9 + [I64] * 10 + [F, I, P, Z, P]
+    lib.vmb_gated_delta_bwd.argtypes = [P] * 15 + [I64] * 10 + [F, I, P, Z, P]
+    lib.vmb_gated_delta_step.argtypes = [P] * 8 + [I64] * 10 + [F, I, P]
+    lib.vmb_gated_delta_workspace_bytes.argtypes = [I] + [I64] * 7 + [I]
+    lib.vmb_axis_rotary_fwd.argtypes = [P] * 7 + [I64] * 9 + [U, F, I, P]
+    lib.vmb_axis_rotary_bwd.argtypes = [P] * 9 + [I64] * 9 + [U, F, I, P]
+    lib.vmb_group_norm_act_fwd.argtypes = [P] * 6 + [I64] * 4 + [F, I, I, P, Z, P]
+    lib.vmb_group_norm_act_bwd.argtypes = [P] * 9 + [I64] * 4 + [I, I, P, Z, P]
+    lib.vmb_group_norm_act_workspace_bytes.argtypes = [I] + [I64] * 4
+    for name in ("vmb_gated_delta_fwd", "vmb_gated_delta_bwd", "vmb_gated_delta_step",
+                 "vmb_axis_rotary_fwd", "vmb_axis_rotary_bwd", "vmb_group_norm_act_fwd",
+                 "vmb_group_norm_act_bwd"):
+        getattr(lib, name).restype = I
+    for name in ("vmb_gated_delta_workspace_bytes", "vmb_group_norm_act_workspace_bytes"):
+        getattr(lib, name).restype = Z
     lib.vmb_status_string.argtypes = [I]
     lib.vmb_status_string.restype = ctypes.c_char_p
     lib.vmb_abi_version.argtypes = []
@@ -377,3 +396,290 @@ def vmb_channel_mean(x: torch.Tensor, xm: torch.Tensor, stream=None) -> torch.Te
     _check(lib.vmb_channel_mean(_f32(x, "x"), _f32(xm, "xm"), batch, channels, L,
                                 _stream(stream)), "vmb_channel_mean")
     return xm
+
+
+# ---------------------------------------------------------------- gated delta rule
+
+def _tokens(t: torch.Tensor, name: str, shape, dtype):
+    """Device address and token stride of a [batch, L, heads, d] tensor whose
+    tokens may be a constant number of elements apart (a view of a wider
+    tensor, such as a slice of one product's output)."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.shape != shape:
+        raise ValueError(f"{name} shape {tuple(t.shape)} != {tuple(shape)}")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a GPU tensor (got {t.device})")
+    batch, L, heads, d = shape
+    s = t.stride()
+    if (d > 1 and s[3] != 1) or (heads > 1 and s[2] != d):
+        raise ValueError(f"{name}: the heads of a token must be contiguous")
+    if L > 1:
+        if batch > 1 and s[0] != L * s[1]:
+            raise ValueError(f"{name}: tokens must be a constant stride apart")
+        return t.data_ptr(), s[1]
+    return t.data_ptr(), s[0] if batch > 1 else heads * d
+
+
+def _full(t: Optional[torch.Tensor], name: str, shape, dtype):
+    """Device address of a contiguous tensor of this shape and dtype, or None."""
+    if t is None:
+        return None
+    if t.shape != shape or t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype} of shape {tuple(shape)} "
+                         f"(got {t.dtype}, {tuple(t.shape)})")
+    return _dev(t, name)
+
+
+def _space(workspace, need: int, device):
+    """The caller's workspace, or one of ``need`` bytes: tensor, address, bytes
+    (SIZE_MAX, sizes that the call itself refuses: none)."""
+    if workspace is None and 0 < need < 1 << 62:
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    if workspace is None:
+        return None, None, 0
+    return workspace, _dev(workspace, "workspace"), workspace.numel() * workspace.element_size()
+
+
+def vmb_gated_delta_workspace_bytes(backward: bool, batch: int, L: int, n_seq: int, heads_k: int,
+                                    heads_v: int, dk: int, dv: int, dtype: torch.dtype) -> int:
+    return int(load_library().vmb_gated_delta_workspace_bytes(
+        int(bool(backward)), batch, L, n_seq, heads_k, heads_v, dk, dv, _DT[dtype]))
+
+
+def _delta_inputs(q, k, v, g, beta, cu_seqlens, scale):
+    """Common checks: the input addresses, the sizes and strides, and the scale."""
+    if q.dim() != 4 or v.dim() != 4:
+        raise ValueError("q, k, v must be [batch, L, heads, d]")
+    batch, L, heads_k, dk = q.shape
+    heads_v, dv = v.shape[2], v.shape[3]
+    dtype = q.dtype
+    _dtype(q, "q")
+    qp, qs = _tokens(q, "q", q.shape, dtype)
+    kp, ks = _tokens(k, "k", q.shape, dtype)
+    vp, vs = _tokens(v, "v", (batch, L, heads_v, dv), dtype)
+    gates = (batch, L, heads_v)
+    gp, bp = _full(g, "g", gates, torch.float32), _full(beta, "beta", gates, torch.float32)
+    n_seq, cu = batch, None
+    if cu_seqlens is not None:
+        n_seq = cu_seqlens.numel() - 1
+        cu = _full(cu_seqlens, "cu_seqlens", (n_seq + 1,), torch.int32)
+    if scale is None:
+        scale = dk ** -0.5
+    return ((qp, kp, vp, gp, bp), cu, (batch, L, n_seq, heads_k, heads_v, dk, dv, qs, ks, vs),
+            float(scale))
+
+
+def vmb_gated_delta_fwd(q, k, v, g, beta, o, scale=None, h0=None, hT=None, cu_seqlens=None,
+                        workspace=None, stream=None):
+    """Gated delta rule over whole sequences: q, k [batch, L, heads_k, dk] and
+    v [batch, L, heads_v, dv] (views with a constant token stride are taken),
+    g, beta float32 [batch, L, heads_v], states float32 [n_seq, heads_v, dk,
+    dv] or None, cu_seqlens int32 [n_seq + 1] or None (scale None: dk^-0.5).
+    Writes o [batch, L, heads_v, dv] and hT; returns o."""
+    lib = _lib or load_library()
+    inputs, cu, sizes, scale = _delta_inputs(q, k, v, g, beta, cu_seqlens, scale)
+    batch, L, n_seq, heads_k, heads_v, dk, dv = sizes[:7]
+    state = (n_seq, heads_v, dk, dv)
+    dt = _DT[q.dtype]
+    need = 0
+    if workspace is None:
+        need = lib.vmb_gated_delta_workspace_bytes(0, *sizes[:7], dt)
+    workspace, wp, wb = _space(workspace, need, q.device)
+    status = lib.vmb_gated_delta_fwd(
+        *inputs, _full(h0, "h0", state, torch.float32), cu,
+        _full(o, "o", (batch, L, heads_v, dv), q.dtype), _full(hT, "hT", state, torch.float32),
+        *sizes, scale, dt, wp, wb, _stream(stream))
+    if status != 0:
+        raise VmbError(status, "vmb_gated_delta_fwd")
+    return o
+
+
+def vmb_gated_delta_bwd(q, k, v, g, beta, do, dq, dk, dv, dg, dbeta, scale=None, h0=None,
+                        dhT=None, dh0=None, cu_seqlens=None, workspace=None, stream=None):
+    """Gradients of vmb_gated_delta_fwd from its inputs and the gradients do of
+    o and dhT of hT (None: zero). Writes dq, dk, dv, dg, dbeta (and dh0 where
+    given), contiguous tensors of the inputs' shapes, and returns them."""
+    lib = _lib or load_library()
+    inputs, cu, sizes, scale = _delta_inputs(q, k, v, g, beta, cu_seqlens, scale)
+    batch, L, n_seq, heads_k, heads_v, d_k, d_v = sizes[:7]
+    state, gates = (n_seq, heads_v, d_k, d_v), (batch, L, heads_v)
+    keys, values = (batch, L, heads_k, d_k), (batch, L, heads_v, d_v)
+    dt = _DT[q.dtype]
+    need = 0
+    if workspace is None:
+        need = lib.vmb_gated_delta_workspace_bytes(1, *sizes[:7], dt)
+    workspace, wp, wb = _space(workspace, need, q.device)
+    f32 = torch.float32
+    status = lib.vmb_gated_delta_bwd(
+        *inputs, _full(h0, "h0", state, f32), cu, _full(do, "do", values, q.dtype),
+        _full(dhT, "dhT", state, f32), _full(dq, "dq", keys, q.dtype),
+        _full(dk, "dk", keys, q.dtype), _full(dv, "dv", values, q.dtype),
+        _full(dg, "dg", gates, f32), _full(dbeta, "dbeta", gates, f32),
+        _full(dh0, "dh0", state, f32), *sizes, scale, dt, wp, wb, _stream(stream))
+    if status != 0:
+        raise VmbError(status, "vmb_gated_delta_bwd")
+    return dq, dk, dv, dg, dbeta
+
+
+def vmb_gated_delta_step(q, k, v, g, beta, state, o, slots=None, scale=None, stream=None):
+    """The recurrence token by token on kept states: q, k [batch, T, heads_k,
+    dk], v, o [batch, T, heads_v, dv], g, beta float32 [batch, T, heads_v];
+    state float32 [n_slots, heads_v, dk, dv] is updated in place, row b in
+    slot slots[b] (int32 [batch]; None: slot b; out of range: row skipped, o
+    zeroed). Returns o."""
+    lib = _lib or load_library()
+    inputs, _, sizes, scale = _delta_inputs(q, k, v, g, beta, None, scale)
+    batch, T, _, heads_k, heads_v, dk, dv = sizes[:7]
+    if state.dim() != 4:
+        raise ValueError("state must be [n_slots, heads_v, dk, dv]")
+    n_slots = state.shape[0]
+    status = lib.vmb_gated_delta_step(
+        *inputs, _full(slots, "slots", (batch,), torch.int32),
+        _full(state, "state", (n_slots, heads_v, dk, dv), torch.float32),
+        _full(o, "o", (batch, T, heads_v, dv), q.dtype), batch, T, n_slots, *sizes[3:], scale,
+        _DT[q.dtype], _stream(stream))
+    if status != 0:
+        raise VmbError(status, "vmb_gated_delta_step")
+    return o
+
+
+# ---------------------------------------------------------------- rotary positions
+
+def _rotary(name, x, yx, pos, inv_freq, sections, y, options, norm_eps, stream, strided):
+    """x: the (first, second or None) tensors that are turned; yx: the forward
+    inputs read by the backward with the norm; y: the outputs."""
+    lib = _lib or load_library()
+    dtype = x[0].dtype
+    dt = _dtype(x[0], "q")
+    if x[0].dim() != 4 or pos.dim() != 3:
+        raise ValueError("heads must be [batch, L, heads, dim], positions [batch, L, n_axes]")
+    batch, L, _, dim = x[0].shape
+    n_axes = len(sections)
+    if pos.shape[2] != n_axes or inv_freq.numel() != sum(sections):
+        raise ValueError("positions hold one axis a section, inv_freq one value a pair")
+    sizes = (ctypes.c_int64 * n_axes)(*sections)
+    ptr, strides, heads, outs = [], [], [], []
+    for i in range(2):
+        if x[i] is None:
+            if y[i] is not None or (yx is not None and yx[i] is not None):
+                raise ValueError("the second tensor is missing")
+            ptr.append((None, None))
+            outs.append(None)
+            strides.append(0)
+            heads.append(0)
+            continue
+        if x[i].dim() != 4:
+            raise ValueError("heads must be [batch, L, heads, dim]")
+        h = x[i].shape[2]
+        shape = (batch, L, h, dim)
+        if strided:
+            xp, ld = _tokens(x[i], "qk"[i], shape, dtype)
+        else:
+            xp, ld = _full(x[i], ("d_yq", "d_yk")[i], shape, dtype), h * dim
+        rp = None
+        if yx is not None and yx[i] is not None:
+            rp, ld = _tokens(yx[i], "qk"[i], shape, dtype)
+        ptr.append((xp, rp))
+        outs.append(_full(y[i], "output", shape, dtype))
+        strides.append(ld)
+        heads.append(h)
+    if norm_eps is not None:
+        options |= VMB_ROTARY_NORM
+    args = [ptr[0][0], ptr[1][0]]
+    if not strided:
+        args += [ptr[0][1], ptr[1][1]]
+    status = getattr(lib, name)(
+        *args, _full(pos, "positions", (pos.shape[0], L, n_axes), torch.int32),
+        _f32(inv_freq, "inv_freq"), ctypes.addressof(sizes), outs[0], outs[1], batch, L, heads[0],
+        heads[1], dim, n_axes, pos.shape[0], strides[0], strides[1], options,
+        0.0 if norm_eps is None else float(norm_eps), dt, _stream(stream))
+    if status != 0:
+        raise VmbError(status, name)
+    return y
+
+
+def vmb_axis_rotary_fwd(q, k, positions, inv_freq, sections, yq, yk, interleaved: bool = False,
+                        norm_eps: Optional[float] = None, stream=None):
+    """Rotary positions with several axes: q, k [batch, L, heads, dim] (views
+    with a constant token stride are taken; k and yk may be None), positions
+    int32 [1 or batch, L, n_axes], inv_freq float32 [pairs], sections the
+    pairs of each axis. norm_eps not None: each head is scaled to unit length
+    first. Writes and returns yq, yk (contiguous)."""
+    return _rotary("vmb_axis_rotary_fwd", (q, k), None, positions, inv_freq, sections, (yq, yk),
+                   VMB_ROTARY_INTERLEAVED if interleaved else 0, norm_eps, stream, True)
+
+
+def vmb_axis_rotary_bwd(d_yq, d_yk, q, k, positions, inv_freq, sections, d_q, d_k,
+                        interleaved: bool = False, norm_eps: Optional[float] = None, stream=None):
+    """Gradients of vmb_axis_rotary_fwd: d_yq, d_yk (contiguous) to d_q, d_k;
+    q and k, the forward inputs, are needed with norm_eps only (else None)."""
+    if norm_eps is not None and (q is None or (d_yk is not None and k is None)):
+        raise ValueError("the norm's backward needs q and k")
+    return _rotary("vmb_axis_rotary_bwd", (d_yq, d_yk), (q, k), positions, inv_freq, sections,
+                   (d_q, d_k), VMB_ROTARY_INTERLEAVED if interleaved else 0, norm_eps, stream,
+                   False)
+
+
+# ---------------------------------------------------------------- group norm
+
+def vmb_group_norm_act_workspace_bytes(backward: bool, batch: int, P: int, channels: int,
+                                       groups: int) -> int:
+    return int(load_library().vmb_group_norm_act_workspace_bytes(int(bool(backward)), batch, P,
+                                                                 channels, groups))
+
+
+def _pixels(x: torch.Tensor):
+    """batch, pixels, channels of a channels-last tensor [batch, ..., channels]."""
+    if x.dim() < 3:
+        raise ValueError(f"x shape {tuple(x.shape)} is not [batch, ..., channels]")
+    batch, channels = x.shape[0], x.shape[-1]
+    return batch, x.numel() // max(1, batch * channels), channels
+
+
+def vmb_group_norm_act_fwd(x, gamma, beta, groups: int, eps: float, act: int, y, mean=None,
+                           rstd=None, workspace=None, stream=None):
+    """Group norm and activation (VMB_ACT_*) on channels-last x [batch, ...,
+    channels]; gamma, beta float32 [channels] or None; mean, rstd float32
+    [batch, groups] or None (outputs that the backward reads). Returns y."""
+    lib = _lib or load_library()
+    batch, P, channels = _pixels(x)
+    c, s, f32 = (channels,), (batch, groups), torch.float32
+    dt = _dtype(x, "x")
+    need = 0
+    if workspace is None:
+        need = lib.vmb_group_norm_act_workspace_bytes(0, batch, P, channels, groups)
+    workspace, wp, wb = _space(workspace, need, x.device)
+    status = lib.vmb_group_norm_act_fwd(
+        _dev(x, "x"), _full(gamma, "gamma", c, f32), _full(beta, "beta", c, f32),
+        _full(y, "y", x.shape, x.dtype), _full(mean, "mean", s, f32), _full(rstd, "rstd", s, f32),
+        batch, P, channels, groups, float(eps), int(act), dt, wp, wb, _stream(stream))
+    if status != 0:
+        raise VmbError(status, "vmb_group_norm_act_fwd")
+    return y
+
+
+def vmb_group_norm_act_bwd(dy, x, gamma, beta, mean, rstd, groups: int, act: int, dx, dgamma=None,
+                           dbeta=None, workspace=None, stream=None):
+    """Gradients of vmb_group_norm_act_fwd from dy, x and the forward call's
+    mean and rstd. Writes dx and, where given, dgamma and dbeta (float32
+    [channels]); returns dx."""
+    lib = _lib or load_library()
+    batch, P, channels = _pixels(x)
+    c, s, f32 = (channels,), (batch, groups), torch.float32
+    dt = _dtype(x, "x")
+    need = 0
+    if workspace is None:
+        need = lib.vmb_group_norm_act_workspace_bytes(1, batch, P, channels, groups)
+    workspace, wp, wb = _space(workspace, need, x.device)
+    status = lib.vmb_group_norm_act_bwd(
+        _full(dy, "dy", x.shape, x.dtype), _dev(x, "x"), _full(gamma, "gamma", c, f32),
+        _full(beta, "beta", c, f32), _full(mean, "mean", s, f32), _full(rstd, "rstd", s, f32),
+        _full(dx, "dx", x.shape, x.dtype), _full(dgamma, "dgamma", c, f32),
+        _full(dbeta, "dbeta", c, f32), batch, P, channels, groups, int(act), dt, wp, wb,
+        _stream(stream))
+    if status != 0:
+        raise VmbError(status, "vmb_group_norm_act_bwd")
+    return dx

@@ -1,0 +1,213 @@
+"""Refusals of the gated delta rule, rotary and group norm entry points on the
+CPU: every bad argument gets its documented status before anything is launched
+(the addresses below are never read)."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2412_16602_amd import vmb
+
+OK, NULL, SHAPE, DTYPE, ALIGN, ALIAS, UNSUP, WS = 0, 1, 2, 3, 4, 5, 6, 7
+F32, BF16 = 0, 1
+NO_GPU = torch.cuda.device_count() == 0
+BASE, STEP = 1 << 40, 1 << 36
+NAN, INF = float("nan"), float("inf")
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not NO_GPU:
+        pytest.skip("fake-pointer validation tests run on CPU-only hosts")
+    return vmb.load_library()
+
+
+def P(i, off=0):
+    return ctypes.c_void_p(BASE + i * STEP + off)
+
+
+def passes(status):
+    assert status in (OK, 8)  # past validation, the launch fails without a GPU
+
+
+def delta(lib, back=False, **kw):
+    a = dict(q=P(0), k=P(1), v=P(2), g=P(3), beta=P(4), h0=P(5), cu=None, o=P(6), hT=P(7),
+             do=P(8), dhT=P(9), dq=P(10), dk_=P(11), dv_=P(12), dg=P(13), db=P(14), dh0=P(15),
+             B=2, L=70, n=2, hk=2, hv=4, dk=32, dv=48, qs=64, ks=64, vs=192, scale=0.1, dt=F32,
+             ws=P(16), wb=1 << 30)
+    a.update(kw)
+    head = [a[x] for x in ("q", "k", "v", "g", "beta", "h0", "cu")]
+    outs = [a[x] for x in (("do", "dhT", "dq", "dk_", "dv_", "dg", "db", "dh0") if back
+                           else ("o", "hT"))]
+    tail = [a[x] for x in ("B", "L", "n", "hk", "hv", "dk", "dv", "qs", "ks", "vs", "scale", "dt",
+                           "ws", "wb")]
+    fn = lib.vmb_gated_delta_bwd if back else lib.vmb_gated_delta_fwd
+    return fn(*head, *outs, *tail, None)
+
+
+@pytest.mark.parametrize("back", [False, True], ids=["fwd", "bwd"])
+@pytest.mark.parametrize("kw,expect", [
+    (dict(q=None), NULL), (dict(k=None), NULL), (dict(v=None), NULL), (dict(g=None), NULL),
+    (dict(beta=None), NULL), (dict(B=0), SHAPE), (dict(L=0), SHAPE), (dict(L=1 << 31), SHAPE),
+    (dict(hk=0), SHAPE), (dict(hk=3), SHAPE), (dict(hv=-4), SHAPE), (dict(dk=0), SHAPE),
+    (dict(n=3), SHAPE), (dict(cu=P(17)), SHAPE), (dict(qs=63), SHAPE), (dict(qs=66), SHAPE),
+    (dict(vs=191), SHAPE), (dict(scale=NAN), SHAPE), (dict(scale=INF), SHAPE),
+    (dict(dk=20), UNSUP), (dict(dk=136, qs=272, ks=272), UNSUP), (dict(dv=264, vs=1056), UNSUP),
+    (dict(dt=2), DTYPE), (dict(q=P(0, 8)), ALIGN), (dict(h0=P(5, 4)), ALIGN),
+    (dict(g=P(3, 2)), ALIGN), (dict(ws=P(16, 8)), ALIGN), (dict(ws=None), WS), (dict(wb=64), WS),
+    (dict(ws=P(1)), ALIAS),
+])
+def test_delta_rejects(lib, back, kw, expect):
+    assert delta(lib, back, **kw) == expect
+
+
+def test_delta_outputs(lib):
+    passes(delta(lib))
+    passes(delta(lib, True))
+    passes(delta(lib, h0=None, hT=None))
+    passes(delta(lib, True, h0=None, dhT=None, dh0=None))
+    passes(delta(lib, B=1, L=70, n=5, cu=P(17)))
+    assert delta(lib, o=None) == NULL and delta(lib, o=P(2)) == ALIAS
+    assert delta(lib, hT=P(5)) == ALIAS and delta(lib, o=P(6, 4)) == ALIGN
+    for x in ("do", "dq", "dk_", "dv_", "dg", "db"):
+        assert delta(lib, True, **{x: None}) == NULL
+    assert delta(lib, True, dq=P(11)) == ALIAS and delta(lib, True, dh0=P(5)) == ALIAS
+    assert delta(lib, True, dg=P(13, 2)) == ALIGN
+    # q, k, v may be slices of one tensor
+    passes(delta(lib, q=P(0), k=P(0, 256), v=P(0, 512), qs=320, ks=320, vs=320))
+
+
+def test_delta_workspace(lib):
+    f = lib.vmb_gated_delta_workspace_bytes
+    small, big = f(0, 2, 70, 2, 2, 4, 32, 48, F32), f(1, 2, 70, 2, 2, 4, 32, 48, F32)
+    assert 0 < small < big
+    assert delta(lib, wb=small - 1) == WS and delta(lib, True, wb=big - 1) == WS
+    none = ctypes.c_size_t(-1).value
+    for bad in ((0, 0, 70, 2, 2, 4, 32, 48, F32), (0, 2, 70, 2, 2, 4, 32, 48, 5),
+                (1, 2, 70, 2, 2, 4, 136, 48, F32), (0, 2, 0, 2, 2, 4, 32, 48, F32),
+                (0, 1 << 30, 1 << 30, 2, 2, 4, 32, 48, F32)):
+        assert f(*bad) == none
+
+
+def step(lib, **kw):
+    a = dict(q=P(0), k=P(1), v=P(2), g=P(3), beta=P(4), slots=P(5), state=P(6), o=P(7), B=3, T=2,
+             n=5, hk=1, hv=2, dk=32, dv=64, qs=32, ks=32, vs=128, scale=0.1, dt=BF16)
+    a.update(kw)
+    return lib.vmb_gated_delta_step(*a.values(), None)
+
+
+@pytest.mark.parametrize("kw,expect", [
+    (dict(q=None), NULL), (dict(state=None), NULL), (dict(o=None), NULL), (dict(T=0), SHAPE),
+    (dict(n=0), SHAPE), (dict(slots=None, n=2), SHAPE), (dict(hv=3, hk=2), SHAPE),
+    (dict(vs=120), SHAPE), (dict(qs=36), SHAPE), (dict(dk=12), UNSUP), (dict(dt=7), DTYPE),
+    (dict(state=P(6, 8)), ALIGN), (dict(slots=P(5, 2)), ALIGN), (dict(o=P(2)), ALIAS),
+    (dict(state=P(0)), ALIAS), (dict(scale=NAN), SHAPE),
+])
+def test_step_rejects(lib, kw, expect):
+    assert step(lib, **kw) == expect
+
+
+def test_step_passes(lib):
+    passes(step(lib))
+    passes(step(lib, slots=None))
+
+
+def rotary(lib, back=False, sections=(8, 8), **kw):
+    a = dict(q=P(0), k=P(1), xq=P(2), xk=P(3), pos=P(4), freq=P(5), yq=P(6), yk=P(7), B=2, L=9,
+             hq=3, hk=1, D=48, axes=len(sections), pb=1, qs=144, ks=48, opt=0, eps=1e-6, dt=BF16)
+    a.update(kw)
+    held = a.pop("sec", (ctypes.c_int64 * len(sections))(*sections))
+    sec = None if held is None else ctypes.addressof(held)
+    names = ["q", "k"] + (["xq", "xk"] if back else []) + ["pos", "freq"]
+    args = [a[x] for x in names] + [sec] + [a[x] for x in (
+        "yq", "yk", "B", "L", "hq", "hk", "D", "axes", "pb", "qs", "ks", "opt", "eps", "dt")]
+    fn = lib.vmb_axis_rotary_bwd if back else lib.vmb_axis_rotary_fwd
+    return fn(*args, None)
+
+
+@pytest.mark.parametrize("back", [False, True], ids=["fwd", "bwd"])
+@pytest.mark.parametrize("kw,expect", [
+    (dict(q=None), NULL), (dict(pos=None), NULL), (dict(freq=None), NULL), (dict(sec=None), NULL),
+    (dict(yq=None), NULL), (dict(yk=None), NULL), (dict(k=None), NULL), (dict(B=0), SHAPE),
+    (dict(L=0), SHAPE), (dict(hq=0), SHAPE), (dict(hk=0), SHAPE), (dict(pb=3), SHAPE),
+    (dict(sections=(0, 0)), SHAPE), (dict(sections=(20, 8)), SHAPE), (dict(sections=(-1, 8)), SHAPE),
+    (dict(sections=(1, 1, 1, 1, 1)), UNSUP), (dict(D=47, qs=141, ks=47), UNSUP),
+    (dict(D=514, qs=1542, ks=514), UNSUP), (dict(opt=4), UNSUP), (dict(dt=3), DTYPE),
+    (dict(q=P(0, 1)), ALIGN), (dict(pos=P(4, 2)), ALIGN), (dict(yq=P(0)), ALIAS),
+    (dict(yk=P(6)), ALIAS), (dict(opt=2, eps=NAN), SHAPE), (dict(opt=2, eps=-1.0), SHAPE),
+])
+def test_rotary_rejects(lib, back, kw, expect):
+    assert rotary(lib, back, **kw) == expect
+
+
+def test_rotary_rules(lib):
+    passes(rotary(lib))
+    passes(rotary(lib, k=None, yk=None, hk=0))
+    passes(rotary(lib, pb=2))
+    assert rotary(lib, qs=143) == SHAPE
+    passes(rotary(lib, True, qs=0, xq=None, xk=None))  # strides count with the norm only
+    assert rotary(lib, True, opt=2, xq=None) == NULL
+    assert rotary(lib, True, opt=2, qs=100) == SHAPE
+    assert rotary(lib, True, opt=2, yq=P(2)) == ALIAS
+    passes(rotary(lib, True, opt=3))
+
+
+def norm(lib, back=False, **kw):
+    a = dict(dy=P(0), x=P(1), ga=P(2), be=P(3), y=P(4), mean=P(5), rstd=P(6), dg=P(7), db=P(8),
+             B=2, pix=9, C=24, G=4, eps=1e-5, act=1, dt=F32, ws=P(9), wb=1 << 30)
+    a.update(kw)
+    if back:
+        names = ("dy", "x", "ga", "be", "mean", "rstd", "y", "dg", "db", "B", "pix", "C", "G",
+                 "act", "dt", "ws", "wb")
+        return lib.vmb_group_norm_act_bwd(*[a[n] for n in names], None)
+    names = ("x", "ga", "be", "y", "mean", "rstd", "B", "pix", "C", "G", "eps", "act", "dt", "ws",
+             "wb")
+    return lib.vmb_group_norm_act_fwd(*[a[n] for n in names], None)
+
+
+@pytest.mark.parametrize("back", [False, True], ids=["fwd", "bwd"])
+@pytest.mark.parametrize("kw,expect", [
+    (dict(x=None), NULL), (dict(y=None), NULL), (dict(rstd=None), NULL), (dict(B=0), SHAPE),
+    (dict(B=70000), SHAPE), (dict(pix=0), SHAPE), (dict(C=0), SHAPE), (dict(G=5), SHAPE),
+    (dict(G=0), SHAPE), (dict(pix=1 << 27), SHAPE), (dict(act=2), UNSUP),
+    (dict(C=16388), UNSUP), (dict(dt=2), DTYPE), (dict(x=P(1, 4)), ALIGN), (dict(y=P(4, 8)), ALIGN),
+    (dict(ga=P(2, 2)), ALIGN), (dict(y=P(1)), ALIAS), (dict(ws=P(1)), ALIAS), (dict(ws=None), WS),
+    (dict(wb=16), WS),
+])
+def test_group_norm_rejects(lib, back, kw, expect):
+    assert norm(lib, back, **kw) == expect
+
+
+def test_group_norm_rules(lib):
+    passes(norm(lib))
+    passes(norm(lib, True))
+    passes(norm(lib, ga=None, be=None, mean=None, rstd=None))
+    passes(norm(lib, True, dg=None, db=None))
+    assert norm(lib, True, dg=None) == NULL and norm(lib, True, mean=None, rstd=None) == NULL
+    for eps in (NAN, INF, -1.0):
+        assert norm(lib, eps=eps) == SHAPE
+    assert norm(lib, mean=P(6)) == ALIAS and norm(lib, True, dg=P(8)) == ALIAS
+    assert (lib.vmb_group_norm_act_workspace_bytes(0, 2, 9, 24, 5)
+            == ctypes.c_size_t(-1).value)
+
+
+def test_python_checks_without_a_gpu():
+    """Shapes, types and strides are refused before any address is taken."""
+    q, v = torch.zeros(1, 4, 2, 8), torch.zeros(1, 4, 2, 16)
+    g = torch.zeros(1, 4, 2)
+    bad = [(q[0], v, g), (q, v[:, :3], g), (q, v, g[..., :1]), (q.double(), v, g),
+           (q, v.bfloat16(), g)]
+    for qq, vv, gg in bad:
+        with pytest.raises(ValueError):
+            vmb.vmb_gated_delta_fwd(qq, qq, vv, gg, gg, torch.zeros_like(vv))
+    with pytest.raises(ValueError, match="GPU tensor"):
+        vmb.vmb_gated_delta_fwd(q, q, v, g, g, torch.zeros_like(v))
+    pos = torch.zeros(1, 4, 2, dtype=torch.int32)
+    freq = torch.zeros(4)
+    for p, f, s in ((pos, freq, (2, 1)), (pos[..., :1], freq, (2, 2)), (pos[0], freq, (2, 2))):
+        with pytest.raises(ValueError):
+            vmb.vmb_axis_rotary_fwd(q, None, p, f, s, torch.zeros_like(q), None)
+    with pytest.raises(ValueError):
+        vmb.vmb_axis_rotary_bwd(q, None, None, None, pos, freq, (2, 2), q, None, norm_eps=1e-6)
+    with pytest.raises(ValueError):
+        vmb.vmb_group_norm_act_fwd(torch.zeros(3, 4), None, None, 2, 1e-5, 0, torch.zeros(3, 4))

@@ -1,0 +1,162 @@
+"""Channels-last group norm with activation against numpy in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from mixer_ref import check, f64, group_norm_ref
+from paper_2412_16602_amd import vmb
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+
+CASES = [  # batch, pixels, channels, groups
+    (1, 1, 1, 1), (2, 1, 8, 8), (1, 49, 192, 32), (3, 50, 200, 5), (2, 33, 7, 7),
+    (1, 9, 30, 3), (2, 3136, 48, 8), (1, 1000, 1536, 4), (5, 17, 2056, 1), (1, 70, 4100, 2),
+    (1, 20000, 24, 24), (40, 5, 64, 16),
+]
+
+
+def make(case, dtype, seed=0, offset=0.5):
+    N, P, C, G = case
+    g = torch.Generator().manual_seed(seed)
+    x = (torch.randn(N, P, C, generator=g) + offset + 0.5 * torch.randn(C, generator=g)).to(dtype)
+    gamma = (1 + 0.1 * torch.randn(C, generator=g)).cuda()
+    beta = (0.1 * torch.randn(C, generator=g)).cuda()
+    return x.cuda(), gamma, beta
+
+
+def run(x, gamma, beta, G, eps, act):
+    y = torch.full_like(x, float("nan"))
+    mean = torch.full((x.shape[0], G), float("nan"), device="cuda")
+    rstd = mean.clone()
+    vmb.vmb_group_norm_act_fwd(x, gamma, beta, G, eps, act, y, mean, rstd)
+    torch.cuda.synchronize()
+    return y, mean, rstd
+
+
+@pytest.mark.parametrize("affine", [True, False], ids=["affine", "bare"])
+@pytest.mark.parametrize("act", [vmb.VMB_ACT_SILU, vmb.VMB_ACT_NONE], ids=["silu", "none"])
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "x".join(map(str, c)))
+def test_forward_and_backward(case, dtype, act, affine):
+    N, P, C, G = case
+    x, gamma, beta = make(case, dtype)
+    if not affine:
+        gamma = beta = None
+    silu = act == vmb.VMB_ACT_SILU
+    eps = 1e-2  # groups of one value: x - mean is 0, and rstd 10
+    y, mean, rstd = run(x, gamma, beta, G, eps, act)
+    ry, rm, rr = group_norm_ref(f64(x), f64(gamma), f64(beta), G, eps, silu)
+    check(y, ry, "y")
+    check(mean, rm, "mean")
+    check(rstd, rr, "rstd")
+    # the backward takes the statistics as given
+    dy = torch.randn(x.shape, generator=torch.Generator().manual_seed(3)).to(dtype).cuda()
+    dx = torch.full_like(x, float("nan"))
+    dgamma, dbeta = torch.full((2, C), float("nan"), device="cuda")
+    vmb.vmb_group_norm_act_bwd(dy, x, gamma, beta, mean, rstd, G, act, dx, dgamma, dbeta)
+    torch.cuda.synchronize()
+    rdx, rdg, rdb = group_norm_ref(f64(x), f64(gamma), f64(beta), G, eps, silu, f64(dy),
+                                   f64(mean), f64(rstd))
+    if C // G * P > 1:  # a group of one value has no gradient: all of it cancels
+        check(dx, rdx, "dx")
+        check(dgamma, rdg, "dgamma")
+    check(dbeta, rdb, "dbeta")
+    dx2 = torch.full_like(x, float("nan"))
+    vmb.vmb_group_norm_act_bwd(dy, x, gamma, beta, mean, rstd, G, act, dx2)
+    torch.cuda.synchronize()
+    assert torch.equal(dx, dx2)
+
+
+@pytest.mark.parametrize("offset", [1e3, -1e4])
+def test_offset_costs_nothing(offset):
+    """x = offset + N(0, 1): centred statistics keep the variance. rstd of x's
+    own float32 values; y is exact to the rounding of x - mean."""
+    x, gamma, beta = make((2, 3000, 64, 8), F32, offset=offset)
+    y, mean, rstd = run(x, gamma, beta, 8, 1e-5, vmb.VMB_ACT_NONE)
+    ry, rm, rr = group_norm_ref(f64(x), f64(gamma), f64(beta), 8, 1e-5, False)
+    check(mean, rm, "mean")
+    check(rstd, rr, "rstd")
+    # the mean's own rounding, 2^-24 |offset|, shifts every value
+    assert np.abs(f64(y) - ry).max() <= 2.0 * 2.0**-23 * abs(offset) + 1e-4
+
+
+def test_one_value_far_out():
+    """A group whose first value is an outlier."""
+    x, gamma, beta = make((1, 500, 32, 4), F32)
+    x[0, 0, 0] = 1e4
+    y, mean, rstd = run(x, gamma, beta, 4, 1e-5, vmb.VMB_ACT_SILU)
+    ry, rm, rr = group_norm_ref(f64(x), f64(gamma), f64(beta), 4, 1e-5, True)
+    check(y, ry, "y")
+    check(rstd, rr, "rstd")
+
+
+def test_constant_groups_and_large_inputs():
+    x = torch.full((1, 100, 16), 3.0, device="cuda")
+    x[..., 8:] = 1e18 * torch.randn(100, 8, device="cuda")
+    y, mean, rstd = run(x, None, None, 2, 1e-5, vmb.VMB_ACT_SILU)
+    assert not y[..., :8].any() and torch.isfinite(y).all()
+    assert mean[0, 0] == 3.0
+
+
+def test_not_finite_stays_in_its_group():
+    x, gamma, beta = make((2, 100, 32, 4), F32)
+    clean, *_ = run(x, gamma, beta, 4, 1e-5, vmb.VMB_ACT_SILU)
+    x[1, 50, 9] = float("inf")
+    y, *_ = run(x, gamma, beta, 4, 1e-5, vmb.VMB_ACT_SILU)
+    assert torch.isnan(y[1, :, 8:16]).any()
+    keep = torch.ones_like(y, dtype=torch.bool)
+    keep[1, :, 8:16] = False
+    assert torch.equal(y[keep], clean[keep])
+
+
+def test_gradient_against_differences():
+    x, gamma, beta = make((2, 21, 12, 3), F32, seed=2)
+    G, eps, act = 3, 1e-3, vmb.VMB_ACT_SILU
+    _, mean, rstd = run(x, gamma, beta, G, eps, act)
+    g = torch.Generator().manual_seed(1)
+    dy = torch.randn(x.shape, generator=g).cuda()
+    dx = torch.empty_like(x)
+    dgamma, dbeta = torch.empty(2, 12, device="cuda")
+    vmb.vmb_group_norm_act_bwd(dy, x, gamma, beta, mean, rstd, G, act, dx, dgamma, dbeta)
+    h = 1e-2  # h^2 / 6 of a third derivative of size 10, and 1e-5 / h of rounding
+    for i, grad in enumerate((dx, dgamma, dbeta)):
+        base = (x, gamma, beta)
+        d = torch.randn(base[i].shape, generator=g).cuda()
+        d /= d.norm()
+        vals = []
+        for sign in (1, -1):
+            p = list(base)
+            p[i] = p[i] + sign * h * d
+            vals.append(float((run(*p, G, eps, act)[0].double() * dy).sum()))
+        want, have = (vals[0] - vals[1]) / (2 * h), float((grad.double() * d).sum())
+        assert abs(want - have) <= 3e-3 * max(1.0, abs(want)), (i, want, have)
+
+
+def test_captured_in_a_graph():
+    x, gamma, beta = make((2, 300, 64, 8), BF16)
+    y, dx = torch.empty_like(x), torch.empty_like(x)
+    mean, rstd = torch.empty(2, 2, 8, device="cuda")
+    dg, db = torch.empty(2, 64, device="cuda")
+    dy = torch.randn(x.shape, device="cuda").to(BF16)
+    ws = torch.empty(vmb.vmb_group_norm_act_workspace_bytes(True, 2, 300, 64, 8),
+                     dtype=torch.uint8, device="cuda")
+
+    def both():
+        vmb.vmb_group_norm_act_fwd(x, gamma, beta, 8, 1e-5, 1, y, mean, rstd, workspace=ws)
+        vmb.vmb_group_norm_act_bwd(dy, x, gamma, beta, mean, rstd, 8, 1, dx, dg, db, workspace=ws)
+
+    both()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both()
+    for _ in range(3):
+        x.copy_(torch.randn(x.shape, device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (y, dx, dg, db)]
+        both()
+        torch.cuda.synchronize()
+        for a, b in zip(got, (y, dx, dg, db)):
+            assert torch.equal(a, b)

@@ -1,0 +1,130 @@
+"""Rotary positions with several axes against numpy in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from mixer_ref import check, f64, rotary_ref
+from paper_2412_16602_amd import vmb
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+
+CASES = [  # batch, L, q heads, k heads, dim, sections, shared positions
+    (1, 1, 1, 1, 2, (1,), True),
+    (2, 49, 3, 1, 64, (16, 16), True),
+    (2, 30, 6, 2, 128, (12, 24, 24), False),   # some of the head passes unturned
+    (1, 33, 2, 0, 48, (5, 8), True),           # odd pairs: no vectors in halves
+    (3, 7, 1, 1, 80, (10, 10, 20), False),
+    (1, 100, 12, 4, 512, (100, 0, 156), True),  # an axis without pairs
+    (1, 5, 1, 1, 510, (255,), True),           # more items than lanes
+]
+
+
+def make(case, dtype, seed=0, reach=100):
+    B, L, hq, hk, D, sections, shared = case
+    g = torch.Generator().manual_seed(seed)
+    wide = torch.randn(B, L, (hq + hk) * D + 8, generator=g).to(dtype).cuda()
+    q = wide[..., :hq * D].unflatten(-1, (hq, D))
+    k = wide[..., hq * D:(hq + hk) * D].unflatten(-1, (hk, D)) if hk else None
+    pos = torch.randint(-reach, reach, (1 if shared else B, L, len(sections)), generator=g,
+                        dtype=torch.int32).cuda()
+    freq = torch.exp(-4 * torch.rand(sum(sections), generator=g)).cuda()
+    return q, k, pos, freq
+
+
+@pytest.mark.parametrize("norm", [None, 1e-6], ids=["plain", "norm"])
+@pytest.mark.parametrize("interleaved", [False, True], ids=["halves", "interleaved"])
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "x".join(map(str, c[:5])))
+def test_forward_and_backward(case, dtype, interleaved, norm):
+    q, k, pos, freq = make(case, dtype)
+    sections = case[5]
+    ys = [torch.full(t.shape, float("nan"), dtype=dtype, device="cuda") if t is not None else None
+          for t in (q, k)]
+    vmb.vmb_axis_rotary_fwd(q, k, pos, freq, sections, *ys, interleaved=interleaved,
+                            norm_eps=norm)
+    torch.cuda.synchronize()
+    p, f = pos.cpu().numpy(), f64(freq)
+    g = torch.Generator().manual_seed(9)
+    for x, y in zip((q, k), ys):
+        if x is not None:
+            check(y, rotary_ref(f64(x), p, f, sections, interleaved, norm), "y")
+    dys = [torch.randn(t.shape, generator=g).to(dtype).cuda() if t is not None else None
+           for t in (q, k)]
+    dxs = [torch.full_like(t, float("nan")) if t is not None else None for t in ys]
+    vmb.vmb_axis_rotary_bwd(*dys, q if norm else None, k if norm else None, pos, freq, sections,
+                            *dxs, interleaved=interleaved, norm_eps=norm)
+    torch.cuda.synchronize()
+    for x, dy, dx in zip((q, k), dys, dxs):
+        if x is not None:
+            check(dx, rotary_ref(f64(x), p, f, sections, interleaved, norm, f64(dy)), "dx")
+
+
+def test_positions_far_out():
+    """Positions to 2^31: the angle is formed in binary64, so the turn stays
+    exact to float32 where binary32 angles would be off by whole turns."""
+    case = (1, 64, 1, 1, 64, (16, 16), True)
+    q, k, pos, freq = make(case, F32, reach=2**31 - 1)
+    y = torch.empty(q.shape, device="cuda")
+    vmb.vmb_axis_rotary_fwd(q, None, pos, freq, (16, 16), y, None)
+    check(y, rotary_ref(f64(q), pos.cpu().numpy(), f64(freq), (16, 16), False, None), "y")
+
+
+def test_gradient_against_differences():
+    case = (1, 9, 2, 0, 16, (3, 4), True)
+    q, _, pos, freq = make(case, F32, seed=4)
+    q = q.contiguous()
+    g = torch.Generator().manual_seed(1)
+    dy, d = (torch.randn(q.shape, generator=g).cuda() for _ in range(2))
+    d /= d.norm()
+    dx, y = torch.empty_like(q), torch.empty_like(q)
+    vmb.vmb_axis_rotary_bwd(dy, None, q, None, pos, freq, (3, 4), dx, None, norm_eps=1e-3)
+    vals = []
+    h = 1e-2  # h^2 / 6 of a third derivative of size 1, and 1e-7 / h of rounding
+    for sign in (1, -1):
+        vmb.vmb_axis_rotary_fwd(q + sign * h * d, None, pos, freq, (3, 4), y, None, norm_eps=1e-3)
+        vals.append(float((y.double() * dy).sum()))
+    want, have = (vals[0] - vals[1]) / (2 * h), float((dx.double() * d).sum())
+    assert abs(want - have) <= 1e-3 * max(1.0, abs(want)), (want, have)
+
+
+def test_zero_heads_and_unaligned():
+    """A head of zeros stays zero with the norm; tensors that are only aligned
+    to their element give what aligned ones give."""
+    B, L, H, D = 1, 17, 2, 64
+    x = torch.randn(B, L, H, D, device="cuda").to(BF16)
+    x[:, 3] = 0
+    pos = torch.arange(2 * L, dtype=torch.int32, device="cuda").view(1, L, 2)
+    freq = torch.rand(32, device="cuda")
+    for inter in (False, True):
+        y = torch.empty_like(x)
+        vmb.vmb_axis_rotary_fwd(x, None, pos, freq, (20, 12), y, None, interleaved=inter,
+                                norm_eps=1e-6)
+        assert not y[:, 3].any()
+        raw = torch.empty(x.numel() + 1, dtype=BF16, device="cuda")
+        odd = raw[1:].view(B, L, H, D)
+        odd.copy_(x)
+        y2 = torch.empty(x.numel() + 1, dtype=BF16, device="cuda")[1:].view(B, L, H, D)
+        vmb.vmb_axis_rotary_fwd(odd, None, pos, freq, (20, 12), y2, None, interleaved=inter,
+                                norm_eps=1e-6)
+        # the norm's sum runs in another order: one rounding may differ
+        check(y2, f64(y), "unaligned")
+
+
+def test_captured_in_a_graph():
+    q, k, pos, freq = make(CASES[1], BF16)
+    y, yk = torch.empty(q.shape, dtype=BF16, device="cuda"), torch.empty(k.shape, dtype=BF16,
+                                                                        device="cuda")
+    vmb.vmb_axis_rotary_fwd(q, k, pos, freq, (16, 16), y, yk)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        vmb.vmb_axis_rotary_fwd(q, k, pos, freq, (16, 16), y, yk)
+    for _ in range(3):
+        q.copy_(torch.randn(q.shape, device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = y.clone()
+        vmb.vmb_axis_rotary_fwd(q, k, pos, freq, (16, 16), y, yk)
+        torch.cuda.synchronize()
+        assert torch.equal(got, y)
