@@ -420,10 +420,10 @@ vmb_status vmb_ss2d_out_norm(const void* y, const void* z, const float* gamma, c
  *   e_t = v_t - S'^T k_t
  *   S_t = S' + beta_t k_t e_t^T
  *   o_t = scale S_t^T q_t
- * The forward and backward calls take whole sequences in chunks of tokens on
- * the matrix cores: binary32 accumulation, inputs of type float32 and every
- * computed operand as sums of two or three bfloat16 values (two, about 16
- * bits, where all outputs of the call are bfloat16).
+ * The forward and backward calls take whole sequences in chunks of 64 tokens
+ * on the matrix cores: binary32 accumulation and state, float32 inputs and
+ * every computed operand as scaled sums of two half-precision values (22 bits;
+ * bfloat16 inputs exactly).
  *
  *   q, k : dtype, [batch, L, heads_k, dk]; v : dtype, [batch, L, heads_v, dv].
  *          A token's heads are contiguous; tokens are q_stride, k_stride,

@@ -5,11 +5,6 @@ namespace vmb {
 namespace delta {
 namespace {
 
-// Planes of the computed operands (state, errors, T, P): three (binary32's 24
-// bits) for binary32 inputs and where a binary32 output hangs on them, two
-// (16 bits) where every output is bfloat16 (8 bits).
-constexpr int kMostPlanes = 3;
-
 int padded_dk(int64_t dk) { return dk <= 32 ? 32 : dk <= 64 ? 64 : 128; }
 
 struct Layout {
@@ -19,8 +14,8 @@ struct Layout {
 
 Layout layout_of(bool backward, int64_t batch, int64_t L, int64_t n_seq, bool packed,
                  int64_t heads_k, int64_t heads_v, int64_t dk, int64_t dv, vmb_dtype dt) {
-    const int64_t C = dt == VMB_BF16 ? Planes<bf16_t>::kChunk : Planes<float>::kChunk;
-    const int64_t nx = dt == VMB_BF16 ? 1 : 3;
+    constexpr int64_t C = kChunk;
+    const int64_t nx = dt == VMB_BF16 ? Planes<bf16_t>::kInput : Planes<float>::kInput;
     Layout o{};
     o.slots = packed ? L / C + n_seq : n_seq * ((L + C - 1) / C);
     size_t at = 0;
@@ -30,7 +25,7 @@ Layout layout_of(bool backward, int64_t batch, int64_t L, int64_t n_seq, bool pa
         return p;
     };
     const size_t ks = static_cast<size_t>(o.slots) * heads_k, vs = static_cast<size_t>(o.slots) * heads_v;
-    const size_t key = ks * C * padded_dk(dk) * nx * 2, tri = vs * C * C * kMostPlanes * 2;
+    const size_t key = ks * C * padded_dk(dk) * nx * 2, tri = vs * kTriSize * kPlanes * 2;
     o.KA = take(key);
     o.QA = take(key);
     o.KT = take(key);
@@ -62,13 +57,13 @@ Sizes sizes_of(const DeltaArgs& a, int64_t slots) {
 Streams streams_of(void* ws, const Layout& o) {
     char* p = static_cast<char*>(ws);
     Streams s;
-    s.KA = reinterpret_cast<__bf16*>(p + o.KA);
-    s.QA = reinterpret_cast<__bf16*>(p + o.QA);
-    s.KT = reinterpret_cast<__bf16*>(p + o.KT);
-    s.QT = reinterpret_cast<__bf16*>(p + o.QT);
-    s.TA = reinterpret_cast<__bf16*>(p + o.TA);
-    s.PA = reinterpret_cast<__bf16*>(p + o.PA);
-    s.TT = reinterpret_cast<__bf16*>(p + o.TT);
+    s.KA = reinterpret_cast<_Float16*>(p + o.KA);
+    s.QA = reinterpret_cast<_Float16*>(p + o.QA);
+    s.KT = reinterpret_cast<_Float16*>(p + o.KT);
+    s.QT = reinterpret_cast<_Float16*>(p + o.QT);
+    s.TA = reinterpret_cast<_Float16*>(p + o.TA);
+    s.PA = reinterpret_cast<_Float16*>(p + o.PA);
+    s.TT = reinterpret_cast<_Float16*>(p + o.TT);
     s.gates = reinterpret_cast<float*>(p + o.gates);
     s.S0 = reinterpret_cast<float*>(p + o.S0);
     s.dS = reinterpret_cast<float*>(p + o.dS);
@@ -77,41 +72,39 @@ Streams streams_of(void* ws, const Layout& o) {
     return s;
 }
 
-template <typename In, int NS, int DK>
+template <typename In, int DK>
 void forward(const DeltaArgs& a, const Sizes& z, const Streams& ws) {
-    constexpr int C = Planes<In>::kChunk;
     const dim3 chunks(static_cast<unsigned>(z.slots), static_cast<unsigned>(z.heads_v));
-    k_delta_prepare<In, NS, DK, false>
-        <<<chunks, C * 4, 0, a.stream>>>(z, a.q, a.k, a.g, a.beta, ws);
+    k_delta_prepare<In, DK, false>
+        <<<chunks, 256, 0, a.stream>>>(z, a.q, a.k, a.g, a.beta, ws);
     const dim3 columns(static_cast<unsigned>(z.n_seq), static_cast<unsigned>(z.heads_v),
                        static_cast<unsigned>((z.dv + 15) / 16));
-    k_delta_walk<In, NS, DK, true, false>
+    k_delta_walk<In, DK, true, false>
         <<<columns, 64, 0, a.stream>>>(z, a.v, a.h0, a.o, a.hT, ws);
 }
 
-template <typename In, int NS, int DK>
+template <typename In, int DK>
 void backward(const DeltaArgs& a, const Sizes& z, const Streams& ws) {
-    constexpr int C = Planes<In>::kChunk;
     const dim3 chunks(static_cast<unsigned>(z.slots), static_cast<unsigned>(z.heads_v));
-    k_delta_prepare<In, NS, DK, true>
-        <<<chunks, C * 4, 0, a.stream>>>(z, a.q, a.k, a.g, a.beta, ws);
+    k_delta_prepare<In, DK, true>
+        <<<chunks, 256, 0, a.stream>>>(z, a.q, a.k, a.g, a.beta, ws);
     const dim3 columns(static_cast<unsigned>(z.n_seq), static_cast<unsigned>(z.heads_v),
                        static_cast<unsigned>((z.dv + 15) / 16));
-    k_delta_walk<In, NS, DK, false, true>
+    k_delta_walk<In, DK, false, true>
         <<<columns, 64, 0, a.stream>>>(z, a.v, a.h0, nullptr, nullptr, ws);
-    k_delta_walk_back<In, NS, DK>
+    k_delta_walk_back<In, DK>
         <<<columns, 64, 0, a.stream>>>(z, a.d_o, a.d_hT, a.d_v, a.d_h0, ws);
     const dim3 keys(static_cast<unsigned>(z.slots), static_cast<unsigned>(z.heads_k));
-    k_delta_grads<In, NS, DK><<<keys, C * 4, 0, a.stream>>>(z, a.q, a.k, a.d_o, a.d_q, a.d_k, a.g,
+    k_delta_grads<In, DK><<<keys, 256, 0, a.stream>>>(z, a.q, a.k, a.d_o, a.d_q, a.d_k, a.g,
                                                             a.h0 == nullptr, a.d_g, a.d_beta, ws);
 }
 
-template <typename In, int NS>
+template <typename In>
 void by_width(const DeltaArgs& a, const Sizes& z, const Streams& ws, bool back) {
     switch (padded_dk(a.dk)) {
-        case 32: back ? backward<In, NS, 32>(a, z, ws) : forward<In, NS, 32>(a, z, ws); break;
-        case 64: back ? backward<In, NS, 64>(a, z, ws) : forward<In, NS, 64>(a, z, ws); break;
-        default: back ? backward<In, NS, 128>(a, z, ws) : forward<In, NS, 128>(a, z, ws);
+        case 32: return back ? backward<In, 32>(a, z, ws) : forward<In, 32>(a, z, ws);
+        case 64: return back ? backward<In, 64>(a, z, ws) : forward<In, 64>(a, z, ws);
+        default: return back ? backward<In, 128>(a, z, ws) : forward<In, 128>(a, z, ws);
     }
 }
 
@@ -122,9 +115,8 @@ vmb_status launch(const DeltaArgs& a, bool back) {
     if (o.slots > (int64_t{1} << 23) || a.n_seq > (int64_t{1} << 23)) return VMB_ERR_UNSUPPORTED;
     const Sizes z = sizes_of(a, o.slots);
     const Streams ws = streams_of(a.ws, o);
-    if (a.dt == VMB_F32) by_width<float, 3>(a, z, ws, back);
-    else if (back || a.hT) by_width<bf16_t, 3>(a, z, ws, back);
-    else by_width<bf16_t, 2>(a, z, ws, back);
+    if (a.dt == VMB_F32) by_width<float>(a, z, ws, back);
+    else by_width<bf16_t>(a, z, ws, back);
     return check_launch();
 }
 

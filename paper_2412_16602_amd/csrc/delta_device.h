@@ -8,29 +8,35 @@
 namespace vmb {
 namespace delta {
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-// One operand fragment (8 values a lane) as a sum of N bfloat16 planes, each
-// the rounding of what the ones before it leave: N = 1 holds a bfloat16 input
-// exactly, 2 hold 16 bits, 3 hold binary32's 24.
+constexpr int kChunk = 64;  // tokens of a chunk
+
+// One operand fragment (8 values a lane) as a sum of N half-precision planes,
+// the second the rounding of what the first leaves: 11 or 22 bits. Operands
+// are scaled by powers of two (per row or per wave) so that their largest
+// value lies in [2^13, 2^14): values down to 2^-17 of it then keep all 22
+// bits, smaller ones an error of 2^-39 of it. Against sums of bfloat16 planes
+// (8 bits each, no scales) this takes 1 product where those take 3, and 3
+// where those take 6.
 template <int N>
 struct Frag {
-    bf16x8 p[N];
+    f16x8 p[N];
 };
+// Planes of every computed operand (state, errors, T, P). One plane, 11 bits,
+// would do for a bfloat16 output's norm but leaves single values off by half
+// of that output's spacing again.
+constexpr int kPlanes = 2;
 
-// c += a b on the matrix cores. Products of planes whose size is below the
-// last plane kept (i + j >= max(NA, NB)) are left out; small ones come first.
+// c += a b on the matrix cores, without the product of the two second planes
+// (2^-22 of the whole); small ones first.
 template <int NA, int NB>
 __device__ __forceinline__ void mma(f32x4& c, const Frag<NA>& a, const Frag<NB>& b) {
-    constexpr int kMost = NA > NB ? NA : NB;
-#pragma unroll
-    for (int s = kMost - 1; s >= 0; --s)
-#pragma unroll
-        for (int i = 0; i < NA; ++i)
-            if (s - i >= 0 && s - i < NB)
-                c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[i], b.p[s - i], c, 0, 0, 0);
+    if constexpr (NA > 1) c = __builtin_amdgcn_mfma_f32_16x16x32_f16(a.p[1], b.p[0], c, 0, 0, 0);
+    if constexpr (NB > 1) c = __builtin_amdgcn_mfma_f32_16x16x32_f16(a.p[0], b.p[1], c, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_f32_16x16x32_f16(a.p[0], b.p[0], c, 0, 0, 0);
 }
 
 // c += a b of binary32 values, 16 x 16 x 4.
@@ -38,24 +44,59 @@ __device__ __forceinline__ void mma_f32(f32x4& c, float a, float b) {
     c = __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
 }
 
+// lo and hi (the two halves of a fragment) times scale.
 template <int N>
-__device__ __forceinline__ void split(const float (&x)[8], Frag<N>& f) {
+__device__ __forceinline__ void split(f32x4 lo, f32x4 hi, float scale, Frag<N>& f) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        float left = x[i];
+        float left = (i < 4 ? lo[i] : hi[i - 4]) * scale;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-            const __bf16 h = static_cast<__bf16>(left);
+            const _Float16 h = static_cast<_Float16>(left);
             f.p[n][i] = h;
             left -= static_cast<float>(h);
         }
     }
 }
-template <int N>
-__device__ __forceinline__ void split(f32x4 lo, f32x4 hi, Frag<N>& f) {
-    const float x[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-    split<N>(x, f);
+
+__device__ __forceinline__ float largest(float m, f32x4 v) {
+    return __builtin_fmaxf(__builtin_fmaxf(__builtin_fmaxf(m, __builtin_fabsf(v[0])),
+                                           __builtin_fmaxf(__builtin_fabsf(v[1]), __builtin_fabsf(v[2]))),
+                           __builtin_fabsf(v[3]));
 }
+
+// The power of two that takes m into [2^13, 2^14) (1 for 0, inf and NaN).
+__device__ __forceinline__ float fitting(float m) {
+    if (!(m > 0.0f && m < __builtin_inff())) return 1.0f;
+    int e = 14 - __builtin_amdgcn_frexp_expf(m);
+    e = e < -100 ? -100 : (e > 100 ? 100 : e);
+    return __builtin_ldexpf(1.0f, e);
+}
+
+// Largest value over the four lanes that share lane % 16, or over the wave.
+__device__ __forceinline__ float over_groups(float m) {
+    m = __builtin_fmaxf(m, __shfl_xor(m, 16));
+    return __builtin_fmaxf(m, __shfl_xor(m, 32));
+}
+__device__ __forceinline__ float over_wave(float m) {
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2) m = __builtin_fmaxf(m, __shfl_xor(m, s));
+    return m;
+}
+
+// A wave's scale for an operand that it forms chunk after chunk: kept while
+// the largest value stays in [2^5, 2^15), which a ballot tells; found anew
+// (a reduction over the wave) only when it leaves that range.
+struct Fit {
+    float up = 1.0f, down = 1.0f;
+    __device__ __forceinline__ void operator()(float m) {
+        const float x = m * up;
+        if (__ballot(!(x < 32768.0f)) != 0 || __ballot(x >= 32.0f) == 0) {
+            up = fitting(over_wave(m));
+            down = 1.0f / up;
+        }
+    }
+};
 
 // The accumulator of a 16 x 16 tile: lane l holds column l % 16, rows
 // 4 (l / 16) + 0..3. Two such tiles, stacked, are an operand of 32 rows for
@@ -63,61 +104,30 @@ __device__ __forceinline__ void split(f32x4 lo, f32x4 hi, Frag<N>& f) {
 // runs in this order ("chained"): lane group g = l / 16 holds 4g + 0..3 and
 // 16 + 4g + 0..3. Every operand that meets one is stored in that order.
 
-// Chained fragment of a row of the inputs: elements k + 4g + 0..3 and
-// k + 16 + 4g + 0..3 of the row at p (valid below d; ok: the row exists).
-__device__ __forceinline__ Frag<1> load_chained(const bf16_t* p, int k, int g, int d, bool ok) {
-    Frag<1> f;
-    bf16x4 a = {}, b = {};
-    const int k0 = k + 4 * g;
-    if (ok && k0 < d) a = *reinterpret_cast<const bf16x4*>(p + k0);
-    if (ok && k0 + 16 < d) b = *reinterpret_cast<const bf16x4*>(p + k0 + 16);
-    f.p[0] = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
-    return f;
+// Four consecutive values of an input row.
+__device__ __forceinline__ f32x4 load4(const bf16_t* p) {
+    typedef unsigned short u16x4 __attribute__((ext_vector_type(4)));
+    const u16x4 x = *reinterpret_cast<const u16x4*>(p);
+    f32x4 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(static_cast<uint32_t>(x[i]) << 16);
+    return v;
 }
-__device__ __forceinline__ Frag<3> load_chained(const float* p, int k, int g, int d, bool ok) {
-    Frag<3> f;
-    f32x4 a = {}, b = {};
-    const int k0 = k + 4 * g;
-    if (ok && k0 < d) a = *reinterpret_cast<const f32x4*>(p + k0);
-    if (ok && k0 + 16 < d) b = *reinterpret_cast<const f32x4*>(p + k0 + 16);
-    split<3>(a, b, f);
-    return f;
+__device__ __forceinline__ f32x4 load4(const float* p) {
+    return *reinterpret_cast<const f32x4*>(p);
 }
 
-// 8 consecutive values of a row (natural order), zeros from d on.
-__device__ __forceinline__ Frag<1> load_row(const bf16_t* p, int k, int d, bool ok) {
-    Frag<1> f;
-    f.p[0] = bf16x8{};
-    if (ok && k < d) f.p[0] = *reinterpret_cast<const bf16x8*>(p + k);
-    return f;
-}
-template <int N>
-__device__ __forceinline__ Frag<N> load_row_f32(const float* p, int k, int d, bool ok) {
-    Frag<N> f;
-    f32x4 a = {}, b = {};
-    if (ok && k < d) {
-        a = *reinterpret_cast<const f32x4*>(p + k);
-        b = *reinterpret_cast<const f32x4*>(p + k + 4);
-    }
-    split<N>(a, b, f);
-    return f;
-}
-__device__ __forceinline__ Frag<3> load_row(const float* p, int k, int d, bool ok) {
-    return load_row_f32<3>(p, k, d, ok);
-}
-
-// Planes of an input operand: a bfloat16 input is one, a binary32 one three.
+// Planes of an input operand: half precision holds a scaled bfloat16 value,
+// and two planes 22 bits of a binary32 one.
 template <typename In>
 struct Planes;
 template <>
 struct Planes<bf16_t> {
     static constexpr int kInput = 1;
-    static constexpr int kChunk = 64;  // tokens of a chunk
 };
 template <>
 struct Planes<float> {
-    static constexpr int kInput = 3;
-    static constexpr int kChunk = 32;
+    static constexpr int kInput = 2;
 };
 
 // Sizes of a call. Chunks live in slots: those of sequence s start at
@@ -138,8 +148,8 @@ struct Span {
 
 // Values of cu_seqlens outside their rule are clamped, so that no token or
 // slot outside the tensors is reached.
-template <int C>
 __device__ __forceinline__ Span span_of(const Sizes& z, int64_t seq) {
+    constexpr int C = kChunk;
     Span s;
     if (!z.cu) {
         s.start = seq * z.L;
@@ -162,8 +172,8 @@ struct Chunk {
     bool first;          // of its sequence
 };
 
-template <int C>
 __device__ __forceinline__ Chunk chunk_of(const Sizes& z, int64_t slot) {
+    constexpr int C = kChunk;
     Chunk c;
     if (!z.cu) {
         const int64_t per = (z.L + C - 1) / C;
@@ -178,10 +188,10 @@ __device__ __forceinline__ Chunk chunk_of(const Sizes& z, int64_t slot) {
     int64_t lo = 0, hi = z.n_seq - 1;
     while (lo < hi) {
         const int64_t mid = (lo + hi + 1) / 2;
-        if (span_of<C>(z, mid).slot0 <= slot) lo = mid;
+        if (span_of(z, mid).slot0 <= slot) lo = mid;
         else hi = mid - 1;
     }
-    const Span s = span_of<C>(z, lo);
+    const Span s = span_of(z, lo);
     const int64_t at = (slot - s.slot0) * C;
     c.seq = lo;
     c.token = s.start + at;
@@ -190,10 +200,24 @@ __device__ __forceinline__ Chunk chunk_of(const Sizes& z, int64_t slot) {
     return c;
 }
 
-// Workspace streams of a (slot, head), all in the fragments' own order (a
-// wave's load of a fragment plane is one contiguous KiB).
-// Gate values of a (slot, value head), C floats each.
-enum Gate { kEg = 0, kBeta = 1, kEnd = 2, kGhi = 3, kGlo = 4, kGates = 5 };
+// Values of a (slot, value head), kChunk floats each. kK, kQ undo the row
+// scales of K and Q; kT, kP those of the triangular operands.
+enum Gate {
+    kEg = 0,     // e^G
+    kBeta = 1,
+    kEnd = 2,    // e^{G_C - G}
+    kGhi = 3,    // G as a sum of two values
+    kGlo = 4,
+    kK = 5,
+    kQ = 6,
+    kEgK = 7,    // e^G kK
+    kEgQ = 8,    // scale e^G kQ
+    kU = 9,      // beta e^{G_C - G} kK
+    kT = 10,
+    kP = 11,
+    kT2 = 12,    // backward: of T^T
+    kGates = 13
+};
 
 }  // namespace delta
 }  // namespace vmb

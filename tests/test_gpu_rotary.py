@@ -107,8 +107,9 @@ def test_zero_heads_and_unaligned():
         y2 = torch.empty(x.numel() + 1, dtype=BF16, device="cuda")[1:].view(B, L, H, D)
         vmb.vmb_axis_rotary_fwd(odd, None, pos, freq, (20, 12), y2, None, interleaved=inter,
                                 norm_eps=1e-6)
-        # the norm's sum runs in another order: one rounding may differ
-        check(y2, f64(y), "unaligned")
+        ref = rotary_ref(f64(x), pos.cpu().numpy(), f64(freq), (20, 12), inter, 1e-6)
+        check(y, ref, "aligned")
+        check(y2, ref, "unaligned")
 
 
 def test_captured_in_a_graph():
