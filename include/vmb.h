@@ -445,7 +445,8 @@ vmb_status vmb_ss2d_out_norm(const void* y, const void* z, const float* gamma, c
  *   hT   : float32, [n_seq, heads_v, dk, dv], the states after the last
  *          tokens (output), or NULL
  *   dk, dv : multiples of 8, dk <= 128, dv <= 256; heads_v a multiple of
- *          heads_k; strides a multiple of 16 bytes
+ *          heads_k; strides a multiple of 16 bytes; strides, heads_k dk and
+ *          heads_v dv at most 2^22 elements
  *   workspace : vmb_gated_delta_workspace_bytes(0, ...) bytes, as for the scan
  * Values that are not finite spread to the other tokens of their chunk (up to
  * 64) in that head, earlier ones included, and to all later ones of their

@@ -8,9 +8,24 @@ namespace {
 int padded_dk(int64_t dk) { return dk <= 32 ? 32 : dk <= 64 ? 64 : 128; }
 
 struct Layout {
-    size_t KA, QA, KT, QT, TA, PA, TT, gates, S0, dS, E, dR, total;
+    size_t KA, QA, KT, QT, TA, PA, TT, gates, S0, dS, E, dR, segM, segN, segS, segD, total;
     int64_t slots;
+    Segments seg;
 };
+
+// Segments of the longest sequence: 1 (none), or as many as bring the walk's
+// waves (of 16 columns) to about two a SIMD. The local walks and the joints
+// more than double the work, so with fewer than eight segments, or segments
+// under eight chunks, they do not pay.
+Segments segments_of(int64_t L, int64_t n_seq, int64_t heads_v, int64_t dv) {
+    const int64_t chunks = (L + kChunk - 1) / kChunk;
+    int64_t segs = 2048 / (n_seq * heads_v * ((dv + 15) / 16));
+    if (segs > chunks / 8) segs = chunks / 8;
+    if (segs < 8) segs = 1;
+    const int64_t each = (chunks + segs - 1) / segs;
+    return Segments{static_cast<uint32_t>((chunks + each - 1) / each), static_cast<uint32_t>(each),
+                    false};
+}
 
 Layout layout_of(bool backward, int64_t batch, int64_t L, int64_t n_seq, bool packed,
                  int64_t heads_k, int64_t heads_v, int64_t dk, int64_t dv, vmb_dtype dt) {
@@ -34,10 +49,20 @@ Layout layout_of(bool backward, int64_t batch, int64_t L, int64_t n_seq, bool pa
     o.PA = take(tri);
     o.TT = take(backward ? tri : 0);
     o.gates = take(vs * kGates * C * 4);
-    o.S0 = take(backward ? vs * dk * dv * 4 : 0);
-    o.dS = take(backward ? vs * dk * dv * 4 : 0);
-    o.E = take(backward ? vs * C * dv * 4 : 0);
-    o.dR = take(backward ? vs * C * dv * 4 : 0);
+    const size_t wide = vs * ((dv + 15) / 16 * 16) * 4;
+    o.S0 = take(backward ? wide * padded_dk(dk) : 0);
+    o.dS = take(backward ? wide * padded_dk(dk) : 0);
+    o.E = take(backward ? wide * C : 0);
+    o.dR = take(backward ? wide * C : 0);
+    o.seg = segments_of(L, n_seq, heads_v, dv);
+    const int64_t units = packed ? o.slots / o.seg.chunks + n_seq
+                                 : (o.slots - 1) / o.seg.chunks + n_seq + o.seg.most;
+    const size_t us = o.seg.most > 1 ? static_cast<size_t>(units) * heads_v * padded_dk(dk) : 0;
+    const size_t cols = (dv + 15) / 16 * 16;
+    o.segM = take(us * padded_dk(dk) * 4);
+    o.segN = take(us * cols * 4);
+    o.segS = take(us * cols * 4);
+    o.segD = take(backward ? us * cols * 4 : 0);
     o.total = at;
     return o;
 }
@@ -45,6 +70,8 @@ Layout layout_of(bool backward, int64_t batch, int64_t L, int64_t n_seq, bool pa
 Sizes sizes_of(const DeltaArgs& a, int64_t slots) {
     Sizes z{};
     z.cu = a.cu;
+    z.per = static_cast<uint32_t>((a.L + kChunk - 1) / kChunk);
+    z.dvp = static_cast<int>((a.dv + 15) / 16 * 16);
     z.L = a.L, z.tokens = a.batch * a.L, z.n_seq = a.n_seq, z.slots = slots;
     z.heads_k = static_cast<int>(a.heads_k), z.heads_v = static_cast<int>(a.heads_v);
     z.group = z.heads_v / z.heads_k;
@@ -69,42 +96,69 @@ Streams streams_of(void* ws, const Layout& o) {
     s.dS = reinterpret_cast<float*>(p + o.dS);
     s.E = reinterpret_cast<float*>(p + o.E);
     s.dR = reinterpret_cast<float*>(p + o.dR);
+    s.segM = reinterpret_cast<float*>(p + o.segM);
+    s.segN = reinterpret_cast<float*>(p + o.segN);
+    s.segS = reinterpret_cast<float*>(p + o.segS);
+    s.segD = reinterpret_cast<float*>(p + o.segD);
     return s;
 }
 
+// A walk's grid: a workgroup of one wave to each of cols tiles of columns (four
+// waves of a head together share what they read in L1, but also its 64 bytes a
+// clock, which then bounds them: 32 x 56x56, 64 x 64 states, 195 against 110 us).
+dim3 walk_grid(const Sizes& z, const Segments& sg, int cols) {
+    return dim3(static_cast<unsigned>(z.n_seq * sg.most), static_cast<unsigned>(z.heads_v),
+                static_cast<unsigned>(cols));
+}
+
+// Starts of all segments: every segment walked from zero and from the
+// identity, then joined.
 template <typename In, int DK>
-void forward(const DeltaArgs& a, const Sizes& z, const Streams& ws) {
-    const dim3 chunks(static_cast<unsigned>(z.slots), static_cast<unsigned>(z.heads_v));
-    k_delta_prepare<In, DK, false>
-        <<<chunks, 256, 0, a.stream>>>(z, a.q, a.k, a.g, a.beta, ws);
-    const dim3 columns(static_cast<unsigned>(z.n_seq), static_cast<unsigned>(z.heads_v),
-                       static_cast<unsigned>((z.dv + 15) / 16));
-    k_delta_walk<In, DK, true, false>
-        <<<columns, 64, 0, a.stream>>>(z, a.v, a.h0, a.o, a.hT, ws);
+void find_starts(const DeltaArgs& a, const Sizes& z, const Segments& sg, const Streams& ws) {
+    const int tiles = z.dvp / 16;
+    k_delta_walk<In, DK, kLocal><<<walk_grid(z, sg, tiles + DK / 16), 64, 0, a.stream>>>(
+        z, sg, a.v, nullptr, nullptr, nullptr, ws);
+    const dim3 joint(static_cast<unsigned>(z.n_seq), static_cast<unsigned>(z.heads_v),
+                     static_cast<unsigned>(tiles));
+    k_delta_join<DK, false><<<joint, DK * 4, 0, a.stream>>>(z, sg, a.h0, ws);
 }
 
 template <typename In, int DK>
-void backward(const DeltaArgs& a, const Sizes& z, const Streams& ws) {
+void forward(const DeltaArgs& a, const Sizes& z, const Segments& sg, const Streams& ws) {
     const dim3 chunks(static_cast<unsigned>(z.slots), static_cast<unsigned>(z.heads_v));
-    k_delta_prepare<In, DK, true>
-        <<<chunks, 256, 0, a.stream>>>(z, a.q, a.k, a.g, a.beta, ws);
-    const dim3 columns(static_cast<unsigned>(z.n_seq), static_cast<unsigned>(z.heads_v),
-                       static_cast<unsigned>((z.dv + 15) / 16));
-    k_delta_walk<In, DK, false, true>
-        <<<columns, 64, 0, a.stream>>>(z, a.v, a.h0, nullptr, nullptr, ws);
-    k_delta_walk_back<In, DK>
-        <<<columns, 64, 0, a.stream>>>(z, a.d_o, a.d_hT, a.d_v, a.d_h0, ws);
+    k_delta_prepare<In, DK, false><<<chunks, 256, 0, a.stream>>>(z, a.q, a.k, a.g, a.beta, ws);
+    if (sg.most > 1) find_starts<In, DK>(a, z, Segments{sg.most, sg.chunks, true}, ws);
+    k_delta_walk<In, DK, kOut><<<walk_grid(z, sg, z.dvp / 16), 64, 0, a.stream>>>(
+        z, sg, a.v, a.h0, a.o, a.hT, ws);
+}
+
+template <typename In, int DK>
+void backward(const DeltaArgs& a, const Sizes& z, const Segments& sg, const Streams& ws) {
+    const dim3 chunks(static_cast<unsigned>(z.slots), static_cast<unsigned>(z.heads_v));
+    k_delta_prepare<In, DK, true><<<chunks, 256, 0, a.stream>>>(z, a.q, a.k, a.g, a.beta, ws);
+    if (sg.most > 1) find_starts<In, DK>(a, z, sg, ws);
+    const dim3 grid = walk_grid(z, sg, z.dvp / 16);
+    k_delta_walk<In, DK, kSave><<<grid, 64, 0, a.stream>>>(z, sg, a.v, a.h0, nullptr, nullptr, ws);
+    if (sg.most > 1) {
+        k_delta_walk_back<In, DK, true><<<grid, 64, 0, a.stream>>>(
+            z, sg, a.d_o, nullptr, nullptr, nullptr, ws);
+        const dim3 joint(static_cast<unsigned>(z.n_seq), static_cast<unsigned>(z.heads_v),
+                         static_cast<unsigned>(z.dvp / 16));
+        k_delta_join<DK, true><<<joint, DK * 4, 0, a.stream>>>(z, sg, a.d_hT, ws);
+    }
+    k_delta_walk_back<In, DK, false><<<grid, 64, 0, a.stream>>>(z, sg, a.d_o, a.d_hT, a.d_v,
+                                                                a.d_h0, ws);
     const dim3 keys(static_cast<unsigned>(z.slots), static_cast<unsigned>(z.heads_k));
     k_delta_grads<In, DK><<<keys, 256, 0, a.stream>>>(z, a.q, a.k, a.d_o, a.d_q, a.d_k, a.g,
-                                                            a.h0 == nullptr, a.d_g, a.d_beta, ws);
+                                                      a.h0 == nullptr, a.d_g, a.d_beta, ws);
 }
 
 template <typename In>
-void by_width(const DeltaArgs& a, const Sizes& z, const Streams& ws, bool back) {
+void by_width(const DeltaArgs& a, const Sizes& z, const Segments& sg, const Streams& ws, bool back) {
     switch (padded_dk(a.dk)) {
-        case 32: return back ? backward<In, 32>(a, z, ws) : forward<In, 32>(a, z, ws);
-        case 64: return back ? backward<In, 64>(a, z, ws) : forward<In, 64>(a, z, ws);
-        default: return back ? backward<In, 128>(a, z, ws) : forward<In, 128>(a, z, ws);
+        case 32: return back ? backward<In, 32>(a, z, sg, ws) : forward<In, 32>(a, z, sg, ws);
+        case 64: return back ? backward<In, 64>(a, z, sg, ws) : forward<In, 64>(a, z, sg, ws);
+        default: return back ? backward<In, 128>(a, z, sg, ws) : forward<In, 128>(a, z, sg, ws);
     }
 }
 
@@ -112,11 +166,11 @@ vmb_status launch(const DeltaArgs& a, bool back) {
     const Layout o = layout_of(back, a.batch, a.L, a.n_seq, a.cu != nullptr, a.heads_k, a.heads_v,
                                a.dk, a.dv, a.dt);
     // a grid's first dimension holds 2^32 threads
-    if (o.slots > (int64_t{1} << 23) || a.n_seq > (int64_t{1} << 23)) return VMB_ERR_UNSUPPORTED;
+    if (o.slots > (int64_t{1} << 23) || a.n_seq > (int64_t{1} << 22)) return VMB_ERR_UNSUPPORTED;
     const Sizes z = sizes_of(a, o.slots);
     const Streams ws = streams_of(a.ws, o);
-    if (a.dt == VMB_F32) by_width<float>(a, z, ws, back);
-    else by_width<bf16_t>(a, z, ws, back);
+    if (a.dt == VMB_F32) by_width<float>(a, z, o.seg, ws, back);
+    else by_width<bf16_t>(a, z, o.seg, ws, back);
     return check_launch();
 }
 

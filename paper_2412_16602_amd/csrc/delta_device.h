@@ -19,7 +19,7 @@ constexpr int kChunk = 64;  // tokens of a chunk
 // are scaled by powers of two (per row or per wave) so that their largest
 // value lies in [2^13, 2^14): values down to 2^-17 of it then keep all 22
 // bits, smaller ones an error of 2^-39 of it. Against sums of bfloat16 planes
-// (8 bits each, no scales) this takes 1 product where those take 3, and 3
+// (8 bits each, no scales) this takes 1 product where those take 2 or 3, and 3
 // where those take 6.
 template <int N>
 struct Frag {
@@ -44,18 +44,69 @@ __device__ __forceinline__ void mma_f32(f32x4& c, float a, float b) {
     c = __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
 }
 
-// lo and hi (the two halves of a fragment) times scale.
+// lo and hi (the two halves of a fragment) times scale, in planes. Two planes
+// take 16 mixed-precision instructions for the 8 values: the product rounded
+// to half precision in its place of the register, then what that leaves. One
+// block, because an instruction that writes half of a register must not be
+// followed at once by one that reads it.
 template <int N>
 __device__ __forceinline__ void split(f32x4 lo, f32x4 hi, float scale, Frag<N>& f) {
+    if constexpr (N == 2) {
+        typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+        unsigned h0, h1, h2, h3, l0, l1, l2, l3;
+        asm("v_fma_mixlo_f16 %0, %8, %16, 0\n"
+            "v_fma_mixlo_f16 %1, %10, %16, 0\n"
+            "v_fma_mixlo_f16 %2, %12, %16, 0\n"
+            "v_fma_mixlo_f16 %3, %14, %16, 0\n"
+            "v_fma_mixhi_f16 %0, %9, %16, 0\n"
+            "v_fma_mixhi_f16 %1, %11, %16, 0\n"
+            "v_fma_mixhi_f16 %2, %13, %16, 0\n"
+            "v_fma_mixhi_f16 %3, %15, %16, 0\n"
+            "v_fma_mixlo_f16 %4, %8, %16, -%0 op_sel:[0,0,0] op_sel_hi:[0,0,1]\n"
+            "v_fma_mixlo_f16 %5, %10, %16, -%1 op_sel:[0,0,0] op_sel_hi:[0,0,1]\n"
+            "v_fma_mixlo_f16 %6, %12, %16, -%2 op_sel:[0,0,0] op_sel_hi:[0,0,1]\n"
+            "v_fma_mixlo_f16 %7, %14, %16, -%3 op_sel:[0,0,0] op_sel_hi:[0,0,1]\n"
+            "v_fma_mixhi_f16 %4, %9, %16, -%0 op_sel:[0,0,1] op_sel_hi:[0,0,1]\n"
+            "v_fma_mixhi_f16 %5, %11, %16, -%1 op_sel:[0,0,1] op_sel_hi:[0,0,1]\n"
+            "v_fma_mixhi_f16 %6, %13, %16, -%2 op_sel:[0,0,1] op_sel_hi:[0,0,1]\n"
+            "v_fma_mixhi_f16 %7, %15, %16, -%3 op_sel:[0,0,1] op_sel_hi:[0,0,1]\n"
+            "s_nop 1\n"
+            : "=&v"(h0), "=&v"(h1), "=&v"(h2), "=&v"(h3), "=&v"(l0), "=&v"(l1), "=&v"(l2),
+              "=&v"(l3)
+            : "v"(lo[0]), "v"(lo[1]), "v"(lo[2]), "v"(lo[3]), "v"(hi[0]), "v"(hi[1]), "v"(hi[2]),
+              "v"(hi[3]), "v"(scale));
+        f.p[0] = __builtin_bit_cast(f16x8, (u32x4{h0, h1, h2, h3}));
+        f.p[1] = __builtin_bit_cast(f16x8, (u32x4{l0, l1, l2, l3}));
+    } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        float left = (i < 4 ? lo[i] : hi[i - 4]) * scale;
+        for (int i = 0; i < 8; ++i)
+            f.p[0][i] = static_cast<_Float16>((i < 4 ? lo[i] : hi[i - 4]) * scale);
+    }
+}
+
+// The same of four values.
+template <int N>
+__device__ __forceinline__ void split4(f32x4 v, float scale, f16x4 (&p)[N]) {
+    if constexpr (N == 2) {
+        typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+        unsigned h0, h1, l0, l1;
+        asm("v_fma_mixlo_f16 %0, %4, %8, 0\n"
+            "v_fma_mixlo_f16 %1, %6, %8, 0\n"
+            "v_fma_mixhi_f16 %0, %5, %8, 0\n"
+            "v_fma_mixhi_f16 %1, %7, %8, 0\n"
+            "s_nop 0\n"
+            "v_fma_mixlo_f16 %2, %4, %8, -%0 op_sel:[0,0,0] op_sel_hi:[0,0,1]\n"
+            "v_fma_mixlo_f16 %3, %6, %8, -%1 op_sel:[0,0,0] op_sel_hi:[0,0,1]\n"
+            "v_fma_mixhi_f16 %2, %5, %8, -%0 op_sel:[0,0,1] op_sel_hi:[0,0,1]\n"
+            "v_fma_mixhi_f16 %3, %7, %8, -%1 op_sel:[0,0,1] op_sel_hi:[0,0,1]\n"
+            "s_nop 1\n"
+            : "=&v"(h0), "=&v"(h1), "=&v"(l0), "=&v"(l1)
+            : "v"(v[0]), "v"(v[1]), "v"(v[2]), "v"(v[3]), "v"(scale));
+        p[0] = __builtin_bit_cast(f16x4, (u32x2{h0, h1}));
+        p[1] = __builtin_bit_cast(f16x4, (u32x2{l0, l1}));
+    } else {
 #pragma unroll
-        for (int n = 0; n < N; ++n) {
-            const _Float16 h = static_cast<_Float16>(left);
-            f.p[n][i] = h;
-            left -= static_cast<float>(h);
-        }
+        for (int i = 0; i < 4; ++i) p[0][i] = static_cast<_Float16>(v[i] * scale);
     }
 }
 
@@ -83,20 +134,6 @@ __device__ __forceinline__ float over_wave(float m) {
     for (int s = 1; s < 64; s *= 2) m = __builtin_fmaxf(m, __shfl_xor(m, s));
     return m;
 }
-
-// A wave's scale for an operand that it forms chunk after chunk: kept while
-// the largest value stays in [2^5, 2^15), which a ballot tells; found anew
-// (a reduction over the wave) only when it leaves that range.
-struct Fit {
-    float up = 1.0f, down = 1.0f;
-    __device__ __forceinline__ void operator()(float m) {
-        const float x = m * up;
-        if (__ballot(!(x < 32768.0f)) != 0 || __ballot(x >= 32.0f) == 0) {
-            up = fitting(over_wave(m));
-            down = 1.0f / up;
-        }
-    }
-};
 
 // The accumulator of a 16 x 16 tile: lane l holds column l % 16, rows
 // 4 (l / 16) + 0..3. Two such tiles, stacked, are an operand of 32 rows for
@@ -136,9 +173,18 @@ struct Planes<float> {
 struct Sizes {
     const int32_t* cu;
     int64_t L, tokens, n_seq, slots;
+    uint32_t per;      // chunks of a sequence of L tokens
+    int dvp;           // dv rounded up to 16: rows of the workspace's E, dR, S0, dS
     int heads_k, heads_v, group, dk, dv;
     int64_t q_stride, k_stride, v_stride;
     float scale;
+};
+
+// Long sequences in segments of chunks chunks, at most `most` a sequence. Their
+// units of workspace are laid out like the slots.
+struct Segments {
+    uint32_t most, chunks;
+    bool skip_last;  // forward: nothing follows the last one
 };
 
 struct Span {
@@ -154,7 +200,7 @@ __device__ __forceinline__ Span span_of(const Sizes& z, int64_t seq) {
     if (!z.cu) {
         s.start = seq * z.L;
         s.len = z.L;
-        s.slot0 = seq * ((z.L + C - 1) / C);
+        s.slot0 = seq * z.per;
         return s;
     }
     int64_t a = z.cu[seq], b = z.cu[seq + 1];
@@ -176,9 +222,9 @@ __device__ __forceinline__ Chunk chunk_of(const Sizes& z, int64_t slot) {
     constexpr int C = kChunk;
     Chunk c;
     if (!z.cu) {
-        const int64_t per = (z.L + C - 1) / C;
-        c.seq = slot / per;
-        const int64_t at = (slot - c.seq * per) * C;
+        const uint32_t seq = static_cast<uint32_t>(slot) / z.per;
+        c.seq = seq;
+        const int64_t at = static_cast<int64_t>(static_cast<uint32_t>(slot) - seq * z.per) * C;
         c.token = c.seq * z.L + at;
         c.n = static_cast<int>(z.L - at < C ? z.L - at : C);
         c.first = at == 0;
@@ -201,22 +247,21 @@ __device__ __forceinline__ Chunk chunk_of(const Sizes& z, int64_t slot) {
 }
 
 // Values of a (slot, value head), kChunk floats each. kK, kQ undo the row
-// scales of K and Q; kT, kP those of the triangular operands.
+// scales of K and Q.
 enum Gate {
     kEg = 0,     // e^G
     kBeta = 1,
     kEnd = 2,    // e^{G_C - G}
-    kGhi = 3,    // G as a sum of two values
+    kGhi = 3,    // G log2(e) as a sum of two values
     kGlo = 4,
     kK = 5,
     kQ = 6,
     kEgK = 7,    // e^G kK
-    kEgQ = 8,    // scale e^G kQ
+    kEgQ = 8,    // scale e^G kQ; forward: times the scale of P
     kU = 9,      // beta e^{G_C - G} kK
-    kT = 10,
+    kT = 10,     // undoes the scale of T, and of P (one value each)
     kP = 11,
-    kT2 = 12,    // backward: of T^T
-    kGates = 13
+    kGates = 12
 };
 
 }  // namespace delta

@@ -11,10 +11,11 @@
 //   X = diag(beta) P^T dO + diag(beta e^{G_C - G}) K dS,   dR = T^T X  (= dV)
 //   dS <- e^{G_C} dS + Q^T diag(scale e^G) dO - K^T diag(e^G) dR.
 // What depends on single chunks alone (T, P, the layouts of K and Q) is made
-// by k_delta_prepare for all chunks at once; the walks over the chunks
-// (k_delta_walk, k_delta_walk_back) hold 16 columns of the state in a wave's
-// registers, and their products chain there: the accumulator tiles of one are
-// the operand of the next, so a walk exchanges nothing between waves.
+// by k_delta_prepare for all chunks at once; then k_delta_walk and
+// k_delta_walk_back go through the chunks with the state. A sequence whose
+// heads are too few to fill the chip is walked in segments: every segment from
+// a zero state and from the identity at once, the results joined one after
+// the other (k_delta_join), then every segment from its true start.
 #pragma once
 
 #include "delta_device.h"
@@ -31,21 +32,29 @@ struct Streams {
     float* gates;                 // per (slot, value head): kGates x C
     float *S0, *dS;               // backward: states before and their gradients behind a chunk
     float *E, *dR;                // backward: [C][dv]
+    // long sequences in segments, per (unit, value head): M [DK][DK], a local
+    // end state, the state at the start and the gradient at the end [DK][dvp]
+    float *segM, *segN, *segS, *segD;
 };
 
+// (addresses as a uniform base and 32 bits a lane, which one instruction takes)
 template <int N>
 __device__ __forceinline__ Frag<N> load_frag(const _Float16* base, int index, int lane) {
     Frag<N> f;
-    const _Float16* p = base + (static_cast<int64_t>(index) * N) * 512 + lane * 8;
+    const uint32_t at = static_cast<uint32_t>(lane) * 16;
 #pragma unroll
-    for (int n = 0; n < N; ++n) f.p[n] = *reinterpret_cast<const f16x8*>(p + n * 512);
+    for (int n = 0; n < N; ++n)
+        f.p[n] = *reinterpret_cast<const f16x8*>(
+            reinterpret_cast<const char*>(base + (index * N + n) * 512) + at);
     return f;
 }
 template <int N>
 __device__ __forceinline__ void store_frag(_Float16* base, int index, int lane, const Frag<N>& f) {
-    _Float16* p = base + (static_cast<int64_t>(index) * N) * 512 + lane * 8;
+    const uint32_t at = static_cast<uint32_t>(lane) * 16;
 #pragma unroll
-    for (int n = 0; n < N; ++n) *reinterpret_cast<f16x8*>(p + n * 512) = f.p[n];
+    for (int n = 0; n < N; ++n)
+        *reinterpret_cast<f16x8*>(reinterpret_cast<char*>(base + (index * N + n) * 512) + at) =
+            f.p[n];
 }
 
 // Fragments of the triangular operands, of row tile t and 32 columns cs of
@@ -70,9 +79,11 @@ __global__ __launch_bounds__(256) void k_delta_prepare(const Sizes z, const void
                                                        const void* kp, const float* gp,
                                                        const float* bp, const Streams ws) {
     constexpr int C = kChunk, NX = Planes<In>::kInput, NS = kPlanes;
-    constexpr int NT = C / 16, KS = DK / 32, CS = C / 32;
-    __shared__ float X[C][C + 1], Tm[C][C + 1];
-    __shared__ float ghi[C], glo[C], sbeta[C], sk[C], sq[C], segd[2][C];
+    constexpr int NT = C / 16, KS = DK / 32, CS = C / 32, MT = DK / 16;
+    // rows of X: a pitch of 68 keeps 16-byte reads aligned and spreads the banks
+    __shared__ __align__(16) float X[C][C + 4];
+    __shared__ __align__(16) float ghi[C], glo[C], sbeta[C], sk[C], sq[C];
+    __shared__ float most_p[NT], most_t[NT];
     __shared__ __align__(16) _Float16 kf[NT * KS * NX * 512], qf[NT * KS * NX * 512];
     const int64_t slot = blockIdx.x;
     const int h = blockIdx.y, hk = h / z.group;
@@ -80,17 +91,36 @@ __global__ __launch_bounds__(256) void k_delta_prepare(const Sizes z, const void
     if (c.n == 0) return;
     const int lane = threadIdx.x % 64, w = threadIdx.x / 64;
     const int col = lane % 16, g = lane / 16;
+    const int mine = 16 * w + col;  // this lane's token
     const int64_t kslot = slot * z.heads_k + hk, vslot = slot * z.heads_v + h;
     const int64_t kbase = kslot * C * DK * NX, pbase = vslot * kTriSize * NS;
     float* gates = ws.gates + vslot * kGates * C;
+    const bool first = h == hk * z.group;
 
+    // this wave's tokens, requested ahead of the gates' sums
+    f32x4 kv[2 * KS], qv[2 * KS];
+    {
+        const In* q = static_cast<const In*>(qp) + (c.token + mine) * z.q_stride +
+                      static_cast<int64_t>(hk) * z.dk + 4 * g;
+        const In* k = static_cast<const In*>(kp) + (c.token + mine) * z.k_stride +
+                      static_cast<int64_t>(hk) * z.dk + 4 * g;
+#pragma unroll
+        for (int i = 0; i < 2 * KS; ++i) {
+            kv[i] = qv[i] = f32x4{};
+            if (mine < c.n && 16 * i + 4 * g < z.dk) {
+                kv[i] = load4(k + 16 * i);
+                qv[i] = load4(q + 16 * i);
+            }
+        }
+    }
     if (w == 0) {
         const int64_t at = (c.token + lane) * z.heads_v + h;
         float gv = lane < c.n ? gp[at] : 0.0f;
         const float bv = lane < c.n ? bp[at] : 0.0f;
-        // exp(-128) is 0 in binary32: no decay is larger, and the sums stay finite
+        // exp(-128) is 0 in binary32: no decay is larger, and the sums stay
+        // finite. In units of log 2, summed in binary64.
         gv = gv < -128.0f ? -128.0f : gv;
-        double G = static_cast<double>(gv);
+        double G = static_cast<double>(gv) * 1.4426950408889634074;
 #pragma unroll
         for (int m = 1; m < C; m *= 2) {
             const double up = __shfl_up(G, m);
@@ -98,36 +128,33 @@ __global__ __launch_bounds__(256) void k_delta_prepare(const Sizes z, const void
         }
         const double end = __shfl(G, C - 1);
         const float hi = static_cast<float>(G), lo = static_cast<float>(G - static_cast<double>(hi));
+        const float eg = fast_exp2(hi), last = fast_exp2(static_cast<float>(end - G));
         ghi[lane] = hi;
         glo[lane] = lo;
         sbeta[lane] = bv;
-        segd[0][lane] = expf(hi);
-        segd[1][lane] = expf(static_cast<float>(end - G));
+        gates[kEg * C + lane] = eg;
+        gates[kBeta * C + lane] = bv;
+        gates[kEnd * C + lane] = last;
+        gates[kGhi * C + lane] = hi;
+        gates[kGlo * C + lane] = lo;
     }
-    // this wave's tokens: rows scaled to their largest value
-    const In* q = static_cast<const In*>(qp) + c.token * z.q_stride + static_cast<int64_t>(hk) * z.dk;
-    const In* k = static_cast<const In*>(kp) + c.token * z.k_stride + static_cast<int64_t>(hk) * z.dk;
-    const bool first = h == hk * z.group;
+    // rows scaled to their largest value
     Frag<NX> kw[KS], qw[KS];
+    float kcol, qcol;
     {
-        const int row = 16 * w + col;
-        f32x4 kv[2 * KS], qv[2 * KS];
         float mk = 0.0f, mq = 0.0f;
 #pragma unroll
         for (int i = 0; i < 2 * KS; ++i) {
-            const int at = 16 * i + 4 * g;
-            kv[i] = qv[i] = f32x4{};
-            if (row < c.n && at < z.dk) {
-                kv[i] = load4(k + row * z.k_stride + at);
-                qv[i] = load4(q + row * z.q_stride + at);
-            }
             mk = largest(mk, kv[i]);
             mq = largest(mq, qv[i]);
         }
-        const float uk = fitting(over_groups(mk)), uq = fitting(over_groups(mq));
+        const float uk = fitting(over_groups(mk)) * 0x1p-14f,  // largest in [1/2, 1)
+                    uq = fitting(over_groups(mq)) * 0x1p-14f;
+        kcol = 1.0f / uk;
+        qcol = 1.0f / uq;
         if (g == 0) {
-            sk[row] = 1.0f / uk;
-            sq[row] = 1.0f / uq;
+            sk[mine] = kcol;
+            sq[mine] = qcol;
         }
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
@@ -135,35 +162,25 @@ __global__ __launch_bounds__(256) void k_delta_prepare(const Sizes z, const void
             split<NX>(qv[2 * ks], qv[2 * ks + 1], uq, qw[ks]);
             store_frag<NX>(kf, w * KS + ks, lane, kw[ks]);
             store_frag<NX>(qf, w * KS + ks, lane, qw[ks]);
-            if (first) {  // once per key head
+        }
+        if (first) {  // once per key head
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
                 store_frag<NX>(ws.KA + kbase, w * KS + ks, lane, kw[ks]);
                 store_frag<NX>(ws.QA + kbase, w * KS + ks, lane, qw[ks]);
             }
         }
     }
     __syncthreads();
-    if (threadIdx.x < C) {
-        const int i = threadIdx.x;
-        const float eg = segd[0][i], end = segd[1][i];
-        gates[kEg * C + i] = eg;
-        gates[kBeta * C + i] = sbeta[i];
-        gates[kEnd * C + i] = end;
-        gates[kGhi * C + i] = ghi[i];
-        gates[kGlo * C + i] = glo[i];
-        gates[kK * C + i] = sk[i];
-        gates[kQ * C + i] = sq[i];
-        gates[kEgK * C + i] = eg * sk[i];
-        gates[kEgQ * C + i] = z.scale * eg * sq[i];
-        gates[kU * C + i] = sbeta[i] * end * sk[i];
-    }
     if (first) {
         // K^T and Q^T: rows of the head, tokens in chained order
 #pragma unroll
         for (int which = 0; which < (kBack ? 2 : 1); ++which) {
             const _Float16* src = which ? qf : kf;
             _Float16* dst = (which ? ws.QT : ws.KT) + kbase;
-            for (int f = w; f < (DK / 16) * CS; f += NT) {
-                const int m = f / CS, cs = f % CS;
+#pragma unroll
+            for (int f = 0; f < MT * CS / NT; ++f) {
+                const int frag = w * (MT * CS / NT) + f, m = frag / CS, cs = frag % CS;
                 // element d = 16 m + col of a token's row lies in fragment m / 2,
                 // lane group d % 16 / 4, place d % 4 + 4 (m % 2)
                 const int at = (m / 2) * NX * 512 + (16 * (col / 4)) * 8 + col % 4 + 4 * (m % 2);
@@ -175,16 +192,16 @@ __global__ __launch_bounds__(256) void k_delta_prepare(const Sizes z, const void
                     for (int n = 0; n < NX; ++n)
                         t.p[n][j] = src[tile * KS * NX * 512 + n * 512 + row * 8 + at];
                 }
-                store_frag<NX>(dst, f, lane, t);
+                store_frag<NX>(dst, frag, lane, t);
             }
         }
     }
 
     // P and M; rows of a tile are the first operand's tokens. Forward: rows j of
     // tile t, columns i of tile w (P by rows as an operand); backward: rows i
-    // of tile t, columns j of tile w (P^T by rows).
-    auto decay = [&](int i, int j) { return expf((ghi[i] - ghi[j]) + (glo[i] - glo[j])); };
-    const float kcol = sk[16 * w + col], qcol = sq[16 * w + col];
+    // of tile t, columns j of tile w (P^T by rows). Everything above the
+    // diagonal is set to 0 by a select.
+    const float chi = ghi[mine], clo = glo[mine], cbeta = sbeta[mine];
     f32x4 p[NT];
     float pm = 0.0f;
 #pragma unroll
@@ -201,14 +218,30 @@ __global__ __launch_bounds__(256) void k_delta_prepare(const Sizes z, const void
                 mma(qk, kt, qw[ks]);
             mma(kk, kt, kw[ks]);
         }
+        const int a0 = 16 * t + 4 * g;
+        const f32x4 rhi = *reinterpret_cast<const f32x4*>(ghi + a0);
+        const f32x4 rlo = *reinterpret_cast<const f32x4*>(glo + a0);
+        const f32x4 rb = *reinterpret_cast<const f32x4*>(sbeta + a0);
+        const f32x4 rk = *reinterpret_cast<const f32x4*>(sk + a0);
+        const f32x4 rq = *reinterpret_cast<const f32x4*>(sq + a0);
+        f32x4 x;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int a = 16 * t + 4 * g + r, b = 16 * w + col;
-            const int i = kBack ? a : b, j = kBack ? b : a;
-            const float d = j <= i ? decay(i, j) : 0.0f;
-            const float unscale = kBack ? sq[a] * kcol : sk[a] * qcol;
-            p[t][r] = j <= i ? z.scale * (qk[r] * unscale) * d * sbeta[j] : 0.0f;
-            X[i][j] = j < i ? (kk[r] * (sk[a] * kcol)) * d * sbeta[j] : 0.0f;
+            const int a = a0 + r;
+            const float up = (rhi[r] - chi) + (rlo[r] - clo);
+            const float d = fast_exp2(kBack ? up : -up);
+            const float beta = kBack ? cbeta : rb[r];
+            const float pv = z.scale * (qk[r] * (kBack ? rq[r] * kcol : rk[r] * qcol)) * d * beta;
+            const float xv = (kk[r] * (rk[r] * kcol)) * d * beta;
+            p[t][r] = (kBack ? mine <= a : a <= mine) ? pv : 0.0f;
+            x[r] = (kBack ? mine < a : a < mine) ? xv : 0.0f;
+        }
+        // X by rows i: forward four neighbouring j of row mine
+        if constexpr (kBack) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) X[a0 + r][mine] = x[r];
+        } else {
+            *reinterpret_cast<f32x4*>(&X[mine][a0]) = x;
         }
         pm = largest(pm, p[t]);
     }
@@ -222,462 +255,791 @@ __global__ __launch_bounds__(256) void k_delta_prepare(const Sizes z, const void
             store_frag<NS>(base, lower ? lower_frag(w, cs) : upper_frag(w, cs), lane, f);
         }
     };
-    {
-        const float up = fitting(over_groups(pm));
-        store_tri(ws.PA + pbase, p, up, !kBack);
-        if (g == 0) gates[kP * C + 16 * w + col] = 1.0f / up;
-    }
+    pm = over_wave(pm);
+    if (lane == 0) most_p[w] = pm;
     __syncthreads();
+    {
+        // one scale for the chunk's P, which the forward walk's gates of Q share
+        float m = most_p[0];
+#pragma unroll
+        for (int i = 1; i < NT; ++i) m = __builtin_fmaxf(m, most_p[i]);
+        const float up = fitting(m);
+        store_tri(ws.PA + pbase, p, up, !kBack);
+        if (w == 1) {
+            const float eg = fast_exp2(ghi[lane]), k1 = sk[lane], q1 = sq[lane];
+            const float end = fast_exp2((ghi[C - 1] - ghi[lane]) + (glo[C - 1] - glo[lane]));
+            gates[kK * C + lane] = k1;
+            gates[kQ * C + lane] = q1;
+            gates[kEgK * C + lane] = eg * k1;
+            gates[kEgQ * C + lane] = z.scale * eg * q1 * (kBack ? 1.0f : up);
+            gates[kU * C + lane] = sbeta[lane] * end * k1;
+            if (lane == 0) gates[kP * C] = 1.0f / up;
+        }
+    }
 
-    if (lane < 16) {
+    // T replaces X block by block. Diagonal blocks: lane c < 16 solves for
+    // column c, from the rows of X that all lanes read alike.
+    {
         float t[16];
+        f32x4 row[16][4];
+#pragma unroll
+        for (int i = 1; i < 16; ++i)
+#pragma unroll
+            for (int q = 0; q <= (i - 1) / 4; ++q)
+                row[i][q] = *reinterpret_cast<const f32x4*>(&X[16 * w + i][16 * w + 4 * q]);
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            float s = i == lane ? 1.0f : 0.0f;
+            float s0 = i == col ? 1.0f : 0.0f, s1 = 0.0f;
 #pragma unroll
-            for (int j = 0; j < i; ++j) s -= X[16 * w + i][16 * w + j] * t[j];
-            t[i] = s;
-            Tm[16 * w + i][16 * w + lane] = s;
+            for (int j = 0; j < i; ++j) {
+                if (j % 2) s1 = __builtin_fmaf(row[i][j / 4][j % 4], t[j], s1);
+                else s0 = __builtin_fmaf(-row[i][j / 4][j % 4], t[j], s0);
+            }
+            t[i] = s0 - s1;
+        }
+        if (lane < 16) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) X[16 * w + i][16 * w + col] = t[i];
+        } else if (lane < 32 && w % 2 == 0) {  // shares a fragment with the diagonal block
+#pragma unroll
+            for (int i = 0; i < 16; ++i) X[16 * w + i][16 * w + 16 + col] = 0.0f;
         }
     }
     __syncthreads();
-    // acc += tile (r, cc) of a times a chained operand tile
-    auto by_tile = [&](f32x4& acc, const float (*a)[C + 1], int r, int cc, f32x4 b) {
+    // acc += tile (r, cc) of X times a chained operand tile
+    auto by_tile = [&](f32x4& acc, int r, int cc, f32x4 b) {
+        const f32x4 a = *reinterpret_cast<const f32x4*>(&X[16 * r + col][16 * cc + 4 * g]);
 #pragma unroll
-        for (int s = 0; s < 4; ++s) mma_f32(acc, a[16 * r + col][16 * cc + 4 * g + s], b[s]);
+        for (int s = 0; s < 4; ++s) mma_f32(acc, a[s], b[s]);
     };
-    auto tile_of = [&](const float (*a)[C + 1], int r, int cc) {
+    auto tile_of = [&](int r, int cc) {
         f32x4 v;
 #pragma unroll
-        for (int s = 0; s < 4; ++s) v[s] = a[16 * r + 4 * g + s][16 * cc + col];
+        for (int s = 0; s < 4; ++s) v[s] = X[16 * r + 4 * g + s][16 * cc + col];
         return v;
     };
     auto put = [&](int r, int cc, f32x4 v) {
 #pragma unroll
-        for (int s = 0; s < 4; ++s) Tm[16 * r + 4 * g + s][16 * cc + col] = -v[s];
+        for (int s = 0; s < 4; ++s) X[16 * r + 4 * g + s][16 * cc + col] = -v[s];
     };
-    if (w < NT / 2) {
+    if (w < NT / 2) {  // one wave a block: it reads what it replaces before
         const int a = 2 * w, b = a + 1;
         f32x4 x = {}, l = {};
-        by_tile(x, X, b, a, tile_of(Tm, a, a));
-        by_tile(l, Tm, b, b, x);
+        by_tile(x, b, a, tile_of(a, a));
+        by_tile(l, b, b, x);
         put(b, a, l);
     }
     __syncthreads();
+    f32x4 l[2] = {};
     if (w < 2) {
-        f32x4 x[2] = {}, l[2] = {};
+        f32x4 x[2] = {};
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-            by_tile(x[r], X, 2 + r, 1, tile_of(Tm, 1, w));
-            if (w == 0) by_tile(x[r], X, 2 + r, 0, tile_of(Tm, 0, w));
+            by_tile(x[r], 2 + r, 1, tile_of(1, w));
+            if (w == 0) by_tile(x[r], 2 + r, 0, tile_of(0, w));
         }
-        by_tile(l[0], Tm, 2, 2, x[0]);
-        by_tile(l[1], Tm, 3, 2, x[0]);
-        by_tile(l[1], Tm, 3, 3, x[1]);
+        by_tile(l[0], 2, 2, x[0]);
+        by_tile(l[1], 3, 2, x[0]);
+        by_tile(l[1], 3, 3, x[1]);
+    }
+    __syncthreads();  // both waves have read the blocks that are replaced
+    if (w < 2) {
         put(2, w, l[0]);
         put(3, w, l[1]);
     }
     __syncthreads();
-    {
-        // T by rows: row 16 w + col, columns 4g + r of tile t
-        f32x4 v[NT];
-        float m = 0.0f;
+    // T by rows: row mine, columns 4g + r of tile t; T^T: row mine, from tile w on
+    f32x4 v[NT];
+    float m = 0.0f;
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int i = 16 * w + col, j = 16 * t + 4 * g + r;
-                v[t][r] = t <= w && j <= i ? Tm[i][j] : 0.0f;
-            }
-            m = largest(m, v[t]);
-        }
-        const float up = fitting(over_groups(m));
-        store_tri(ws.TA + pbase, v, up, true);
-        if (g == 0) gates[kT * C + 16 * w + col] = 1.0f / up;
+    for (int t = 0; t < NT; ++t) {
+        v[t] = f32x4{};
+        if (t <= (w | 1)) v[t] = *reinterpret_cast<const f32x4*>(&X[mine][16 * t + 4 * g]);
+        m = largest(m, v[t]);
     }
+    m = over_wave(m);
+    if (lane == 0) most_t[w] = m;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < NT; ++i) m = __builtin_fmaxf(m, most_t[i]);
+    // T's diagonal is 1: as it is, unless it does not fit half precision
+    const float up = m < 32768.0f ? 1.0f : fitting(m);
+    store_tri(ws.TA + pbase, v, up, true);
+    if (threadIdx.x == 0) gates[kT * C] = 1.0f / up;
     if constexpr (kBack) {
-        f32x4 v[NT];
-        float m = 0.0f;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int i = 16 * t + 4 * g + r, j = 16 * w + col;
-                v[t][r] = t >= w && j <= i ? Tm[i][j] : 0.0f;
-            }
-            m = largest(m, v[t]);
+            v[t] = f32x4{};
+            if (t >= w) v[t] = tile_of(t, w);
         }
-        const float up = fitting(over_groups(m));
         store_tri(ws.TT + pbase, v, up, false);
-        if (g == 0) gates[kT2 * C + 16 * w + col] = 1.0f / up;
     }
 }
 
 // --------------------------------------------------------------------- walk
+
+// What the walks find in common: their part of the work.
+struct Part {
+    int64_t seq, unit, start, slot0, c0, c1, len;
+    bool first, last;  // of the sequence
+};
+
+// A segment of a sequence: blockIdx.x counts the segments of every sequence.
+__device__ __forceinline__ bool part_of(const Sizes& z, const Segments& sg, Part& p) {
+    const uint32_t seq = blockIdx.x / sg.most, seg = blockIdx.x - seq * sg.most;
+    const Span span = span_of(z, seq);
+    const int64_t chunks = (span.len + kChunk - 1) / kChunk;
+    p.seq = seq;
+    p.start = span.start;
+    p.slot0 = span.slot0;
+    p.len = span.len;
+    p.unit = span.slot0 / sg.chunks + seq + seg;
+    p.c0 = static_cast<int64_t>(seg) * sg.chunks;
+    p.c1 = p.c0 + sg.chunks < chunks ? p.c0 + sg.chunks : chunks;
+    p.first = seg == 0;
+    p.last = p.c1 == chunks;
+    return p.first || p.c0 < chunks;
+}
+
+// One column of a chunk's 64 tokens, this lane's rows 16 t + 4 g + r: byte
+// offsets from the chunk's first token (sizes keep 64 tokens under 2 GiB).
+struct Column {
+    uint32_t at[kChunk / 16][4];
+    __device__ __forceinline__ Column(uint32_t stride, uint32_t g, uint32_t col, uint32_t size) {
+#pragma unroll
+        for (int t = 0; t < kChunk / 16; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) at[t][r] = ((16 * t + 4 * g + r) * stride + col) * size;
+    }
+};
+// Unconverted values (a conversion next to its load would make each load wait
+// for the last); left: tokens from the chunk's first to the sequence's end,
+// zeros behind it.
+template <typename In>
+__device__ __forceinline__ void load_column(In (&x)[kChunk / 16][4], const In* p,
+                                            const Column& c, int64_t left, int g) {
+    const char* base = reinterpret_cast<const char*>(p);
+    if (left >= kChunk) {
+#pragma unroll
+        for (int t = 0; t < kChunk / 16; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[t][r] = *reinterpret_cast<const In*>(base + c.at[t][r]);
+    } else {
+#pragma unroll
+        for (int t = 0; t < kChunk / 16; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                x[t][r] = In{};
+                if (16 * t + 4 * g + r < left)
+                    x[t][r] = *reinterpret_cast<const In*>(base + c.at[t][r]);
+            }
+    }
+}
+template <typename In>
+__device__ __forceinline__ void store_column(In* p, const Column& c, const f32x4 (&x)[kChunk / 16],
+                                             int64_t left, int g) {
+    char* base = reinterpret_cast<char*>(p);
+    if (left >= kChunk) {
+#pragma unroll
+        for (int t = 0; t < kChunk / 16; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                *reinterpret_cast<In*>(base + c.at[t][r]) = from_f32<In>(x[t][r]);
+    } else {
+#pragma unroll
+        for (int t = 0; t < kChunk / 16; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (16 * t + 4 * g + r < left)
+                    *reinterpret_cast<In*>(base + c.at[t][r]) = from_f32<In>(x[t][r]);
+    }
+}
+// Tiles of the workspace, padded rows pitch apart (at: this lane's first, bytes).
+template <int TILES>
+__device__ __forceinline__ void store_tiles(float* base, uint32_t at, int pitch,
+                                            const f32x4 (&x)[TILES], float scale) {
+#pragma unroll
+    for (int t = 0; t < TILES; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            *reinterpret_cast<float*>(reinterpret_cast<char*>(base + (16 * t + r) * pitch) + at) =
+                x[t][r] * scale;
+}
 
 template <int N, int COUNT>
 __device__ __forceinline__ void fetch(Frag<N> (&f)[COUNT], const _Float16* base, int lane) {
 #pragma unroll
     for (int i = 0; i < COUNT; ++i) f[i] = load_frag<N>(base, i, lane);
 }
+template <int TILES>
+__device__ __forceinline__ float largest_of(const f32x4 (&x)[TILES]) {
+    float m = 0.0f;
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) m = largest(m, x[t]);
+    return m;
+}
+template <int TILES>
+__device__ __forceinline__ void times(f32x4 (&x)[TILES], float f) {
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) x[t] *= f;
+}
 
-// One wave: 16 columns of one head's state through its sequence. kOut: write
-// o; kSave: keep each chunk's entry state and errors for the backward pass.
-// The operands of the next chunk are requested as soon as this one's are used.
-template <typename In, int DK, bool kOut, bool kSave>
-__global__ __launch_bounds__(64, 1) void k_delta_walk(const Sizes z, const void* vp,
-                                                      const float* h0, void* op, float* hT,
-                                                      const Streams ws) {
+// The scale of a wave's operands, state included: everything the wave holds is
+// `up` times its value. Kept while the largest value of a chunk stays in
+// [2^5, 2^15), which ballots tell; values down to 2^-8 of it keep 22 bits,
+// smaller ones an error of 2^-30 of it.
+struct Scale {
+    float up = 1.0f;
+    // Whether m, a lane's largest value, is too large for half precision.
+    __device__ __forceinline__ static bool over(float m) { return __ballot(!(m < 32768.0f)) != 0; }
+    // The factor that brings the wave's largest value into [2^9, 2^10).
+    __device__ __forceinline__ static float factor(float m) {
+        return fitting(over_wave(m)) * 0x1p-4f;
+    }
+    // A chunk's largest value: too small, and not all zeros.
+    __device__ __forceinline__ static bool under(float m) {
+        return __ballot(m >= 32.0f) == 0 && __ballot(m > 0.0f) != 0;
+    }
+};
+
+// The walks: a wave takes 16 columns of a head's state through the chunks of a
+// segment (a whole sequence, or a part of a long one) and shares nothing. The
+// operands of the next chunk are requested as soon as this one's are used. A
+// chunk of 64 x 64 states takes about 450 vector instructions, 84 of them
+// matrix products, and 48 loads of a KiB; bound by that issue rate and, from
+// about four waves a compute unit on, by the 64 bytes a clock of L1. Measured:
+// 2.2 us a chunk. (Four waves a column tile, each a quarter of the rows, with
+// the tiles exchanged through LDS, took 1.7 times the instructions and twice
+// the time.)
+// kOut: write o and hT. kSave: keep each chunk's entry state and errors for the
+// backward pass. kLocal: a segment's end state from a zero start, and, in DK
+// further columns, from the identity without values, which is the matrix that
+// takes any start through it.
+enum WalkKind { kOut, kSave, kLocal };
+
+template <typename In, int DK, WalkKind kKind>
+__global__ __launch_bounds__(64, 1) void k_delta_walk(const Sizes z, const Segments sg,
+                                                       const void* vp, const float* h0, void* op,
+                                                       float* hT, const Streams ws) {
     constexpr int C = kChunk, NX = Planes<In>::kInput, NS = kPlanes;
     constexpr int NT = C / 16, KS = DK / 32, CS = C / 32, MT = DK / 16;
-    const int lane = threadIdx.x % 64, g = lane / 16;
-    const int64_t seq = blockIdx.x;
+    // operands that fit the registers are requested a chunk ahead, others a
+    // product or two
+    constexpr bool kAhead = DK * NX <= (kKind == kOut ? 64 : 128);
+    Part part;
+    if (!part_of(z, sg, part) || (kKind == kLocal && part.last && sg.skip_last)) return;
+    const int lane = threadIdx.x, g = lane / 16;
+    const int ct = blockIdx.z, tiles = z.dvp / 16;
     const int h = blockIdx.y, hk = h / z.group;
-    const int col = blockIdx.z * 16 + lane % 16;
-    const bool on = col < z.dv;
-    const Span span = span_of(z, seq);
-    const int64_t state = (seq * z.heads_v + h) * z.dk * z.dv + col;
-    f32x4 S[MT];
+    const int col = ct * 16 + lane % 16;
+    const bool on = col < z.dv;                           // a column of v
+    const bool blind = kKind == kLocal && ct >= tiles;    // of the identity
+    const int64_t step = static_cast<int64_t>(z.heads_v) * z.dv;
+    const int64_t unit = part.unit * z.heads_v + h;
+    const int64_t state = (part.seq * z.heads_v + h) * z.dk * z.dv + col;
+    const uint32_t tile_at = static_cast<uint32_t>(4 * g * z.dvp + col) * 4;
+
+    f32x4 S[MT];  // times scale.up, like R, E and U
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int row = 16 * m + 4 * g + r;
-            S[m][r] = h0 && on && row < z.dk ? h0[state + row * z.dv] : 0.0f;
+            float x = 0.0f;
+            if (kKind == kLocal) {
+                x = row == col - z.dvp ? 1.0f : 0.0f;
+            } else if (part.first) {
+                if (h0 && on && row < z.dk) x = h0[state + row * z.dv];
+            } else {
+                x = ws.segS[(unit * DK + row) * z.dvp + col];
+            }
+            S[m][r] = x;
         }
-    const In* v = static_cast<const In*>(vp) + span.start * z.v_stride +
-                  static_cast<int64_t>(h) * z.dv + (on ? col : 0);
-    In* o = static_cast<In*>(op) + (span.start * z.heads_v + h) * z.dv + col;
-    const int64_t o_step = static_cast<int64_t>(z.heads_v) * z.dv;
-    const int64_t chunks = (span.len + C - 1) / C;
+    // lanes past the last column repeat the first one
+    const In* v = static_cast<const In*>(vp) + part.start * z.v_stride + static_cast<int64_t>(h) * z.dv;
+    In* o = static_cast<In*>(op) + part.start * step + static_cast<int64_t>(h) * z.dv;
+    const Column vc(static_cast<uint32_t>(z.v_stride), g, on ? col : 0, sizeof(In)),
+        oc(static_cast<uint32_t>(step), g, col, sizeof(In));
 
-    Frag<NX> ka[NT * KS], qa[kOut ? NT * KS : 1], kt[MT * CS];
-    Frag<NS> ta[kTri], pa[kOut ? kTri : 1];
-    In vr[NT][4];
-    auto kbase = [&](int64_t ci) { return ((span.slot0 + ci) * z.heads_k + hk) * C * DK * NX; };
-    auto pbase = [&](int64_t ci) { return ((span.slot0 + ci) * z.heads_v + h) * kTriSize * NS; };
+    Frag<NX> ka[NT * KS], qa[kKind == kOut ? NT * KS : 1], kt[MT * CS];
+    Frag<NS> ta[kTri], pa[kKind == kOut ? kTri : 1];
+    In vr[NT][4] = {};
+    f32x4 egk[NT], egq[NT], gu[NT];
+    float last = 0.0f, psc = 0.0f, tsc = 0.0f;
+    auto kbase = [&](int64_t ci) { return ((part.slot0 + ci) * z.heads_k + hk) * C * DK * NX; };
+    auto vslot = [&](int64_t ci) { return (part.slot0 + ci) * z.heads_v + h; };
+    auto gate = [&](int64_t ci, int which, f32x4 (&x)[NT]) {
+        const char* p = reinterpret_cast<const char*>(ws.gates + (vslot(ci) * kGates + which) * C);
+        const uint32_t at = static_cast<uint32_t>(g) * 16;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) x[t] = *reinterpret_cast<const f32x4*>(p + 64 * t + at);
+    };
+    auto fetch_k = [&](int64_t ci) { fetch(ka, ws.KA + kbase(ci), lane); };
     auto fetch_v = [&](int64_t ci) {
+        if (!blind) load_column(vr, v + ci * C * z.v_stride, vc, part.len - ci * C, g);
+        gate(ci, kEgK, egk);
+    };
+    auto fetch_t = [&](int64_t ci) {
+        fetch(ta, ws.TA + vslot(ci) * kTriSize * NS, lane);
+        tsc = ws.gates[(vslot(ci) * kGates + kT) * C];
+    };
+    auto fetch_q = [&](int64_t ci) {
+        fetch(qa, ws.QA + kbase(ci), lane);
+        gate(ci, kEgQ, egq);
+    };
+    auto fetch_p = [&](int64_t ci) {
+        fetch(pa, ws.PA + vslot(ci) * kTriSize * NS, lane);
+        psc = ws.gates[(vslot(ci) * kGates + kP) * C];
+    };
+    auto fetch_s = [&](int64_t ci) {
+        fetch(kt, ws.KT + kbase(ci), lane);
+        gate(ci, kU, gu);
+        last = ws.gates[(vslot(ci) * kGates + kEg) * C + C - 1];
+    };
+    if (part.c0 < part.c1) {
+        fetch_v(part.c0);
+        fetch_k(part.c0);
+        if constexpr (kAhead) {
+            fetch_t(part.c0);
+            if constexpr (kKind == kOut) {
+                fetch_q(part.c0);
+                fetch_p(part.c0);
+            }
+            fetch_s(part.c0);
+        }
+    }
+    Scale s;
+    {
+        float m = largest_of(S);
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                int64_t row = ci * C + 16 * t + 4 * g + r;
-                row = row < span.len ? row : span.len - 1;  // masked where it is used
-                vr[t][r] = v[row * z.v_stride];
-            }
-    };
-    if (chunks > 0) {
-        fetch(ka, ws.KA + kbase(0), lane);
-        fetch_v(0);
-        fetch(ta, ws.TA + pbase(0), lane);
-        if constexpr (kOut) {
-            fetch(qa, ws.QA + kbase(0), lane);
-            fetch(pa, ws.PA + pbase(0), lane);
-        }
-        fetch(kt, ws.KT + kbase(0), lane);
+            for (int r = 0; r < 4; ++r) m = __builtin_fmaxf(m, __builtin_fabsf(to_f32(vr[t][r])));
+        s.up = Scale::factor(m);
+        times(S, s.up);
     }
-    Fit fs, fr, fe, fu;
-    for (int64_t ci = 0; ci < chunks; ++ci) {
-        const int64_t next = ci + 1 < chunks ? ci + 1 : ci;
-        const int n = static_cast<int>(span.len - ci * C < C ? span.len - ci * C : C);
-        const int64_t vslot = (span.slot0 + ci) * z.heads_v + h;
-        const float* gates = ws.gates + vslot * kGates * C;
-        f32x4 egk[NT], egq[NT], gt[NT], gpp[NT], gu[NT];
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            const float* p = gates + 16 * t + 4 * g;
-            egk[t] = *reinterpret_cast<const f32x4*>(p + kEgK * C);
-            gt[t] = *reinterpret_cast<const f32x4*>(p + kT * C);
-            gu[t] = *reinterpret_cast<const f32x4*>(p + kU * C);
-            if constexpr (kOut) {
-                egq[t] = *reinterpret_cast<const f32x4*>(p + kEgQ * C);
-                gpp[t] = *reinterpret_cast<const f32x4*>(p + kP * C);
-            }
+    for (int64_t ci = part.c0; ci < part.c1; ++ci) {
+        const int64_t next = ci + 1 < part.c1 ? ci + 1 : ci;
+        float m = largest_of(S), most = m;
+        if (Scale::over(m)) {
+            const float f = Scale::factor(m);
+            times(S, f);
+            s.up *= f;
         }
-        const float last = gates[kEg * C + C - 1];
-        if constexpr (kSave) {
-            float* s0 = ws.S0 + vslot * z.dk * z.dv + col;
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int row = 16 * m + 4 * g + r;
-                    if (on && row < z.dk) s0[row * z.dv] = S[m][r];
-                }
+        if constexpr (kKind == kSave)
+            store_tiles(ws.S0 + vslot(ci) * DK * z.dvp, tile_at, z.dvp, S, 1.0f / s.up);
+        if constexpr (!kAhead) {
+            fetch_t(ci);
+            if constexpr (kKind == kOut) fetch_q(ci);
         }
-        float m = 0.0f;
-#pragma unroll
-        for (int i = 0; i < MT; ++i) m = largest(m, S[i]);
-        fs(m);
+        // R = V - e^G K S
         Frag<NS> sf[KS];
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) split<NS>(S[2 * ks], S[2 * ks + 1], fs.up, sf[ks]);
+        for (int ks = 0; ks < KS; ++ks) split<NS>(S[2 * ks], S[2 * ks + 1], 1.0f, sf[ks]);
         f32x4 R[NT], O[NT];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             f32x4 acc = {};
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) mma(acc, ka[t * KS + ks], sf[ks]);
+            acc *= egk[t];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const float x = on && 16 * t + 4 * g + r < n ? to_f32(vr[t][r]) : 0.0f;
-                R[t][r] = x - egk[t][r] * (acc[r] * fs.down);
-            }
+            for (int r = 0; r < 4; ++r) R[t][r] = __builtin_fmaf(to_f32(vr[t][r]), s.up, -acc[r]);
         }
-        fetch(ka, ws.KA + kbase(next), lane);
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (kAhead) fetch_k(next);
         fetch_v(next);
-        if constexpr (kOut) {
+        if constexpr (kKind == kOut) {
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
                 O[t] = f32x4{};
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) mma(O[t], qa[t * KS + ks], sf[ks]);
-                O[t] *= egq[t] * fs.down;
+                O[t] *= egq[t];
             }
-            fetch(qa, ws.QA + kbase(next), lane);
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (kAhead) fetch_q(next);
+            else fetch_p(ci);
         }
-        m = 0.0f;
-#pragma unroll
-        for (int t = 0; t < NT; ++t) m = largest(m, R[t]);
-        fr(m);
+        if constexpr (!kAhead) fetch_s(ci);
+        m = largest_of(R);
+        most = __builtin_fmaxf(most, m);
+        auto rescale = [&](f32x4 (&x)[NT], float top) {  // the rest of what is held with it
+            const float f = Scale::factor(top);
+            times(x, f);
+            times(S, f);
+            if constexpr (kKind == kOut) times(O, f);
+            s.up *= f;
+        };
+        if (Scale::over(m)) rescale(R, m);
+        // E = T R
         Frag<NS> rf[CS];
 #pragma unroll
-        for (int cs = 0; cs < CS; ++cs) split<NS>(R[2 * cs], R[2 * cs + 1], fr.up, rf[cs]);
+        for (int cs = 0; cs < CS; ++cs) split<NS>(R[2 * cs], R[2 * cs + 1], 1.0f, rf[cs]);
         f32x4 E[NT];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             E[t] = f32x4{};
 #pragma unroll
             for (int cs = 0; cs <= t / 2; ++cs) mma(E[t], ta[lower_frag(t, cs)], rf[cs]);
-            E[t] *= gt[t] * fr.down;
         }
-        fetch(ta, ws.TA + pbase(next), lane);
-        if constexpr (kSave) {
-            float* e = ws.E + vslot * C * z.dv + col;
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (on) e[(16 * t + 4 * g + r) * z.dv] = E[t][r];
-        }
-        if constexpr (kOut) {
-            m = 0.0f;
-#pragma unroll
-            for (int t = 0; t < NT; ++t) m = largest(m, E[t]);
-            fe(m);
+        if (tsc != 1.0f) times(E, tsc);
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (kAhead) fetch_t(next);
+        m = largest_of(E);
+        most = __builtin_fmaxf(most, m);
+        if (Scale::over(m)) rescale(E, m);
+        if constexpr (kKind == kSave)
+            store_tiles(ws.E + vslot(ci) * C * z.dvp, tile_at, z.dvp, E, 1.0f / s.up);
+        // O = scale e^G Q S + P diag(beta) E
+        if constexpr (kKind == kOut) {
             Frag<NS> ef[CS];
 #pragma unroll
-            for (int cs = 0; cs < CS; ++cs) split<NS>(E[2 * cs], E[2 * cs + 1], fe.up, ef[cs]);
+            for (int cs = 0; cs < CS; ++cs) split<NS>(E[2 * cs], E[2 * cs + 1], 1.0f, ef[cs]);
+            const float down = psc / s.up;  // the gates of Q hold P's scale
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
-                f32x4 acc = {};
 #pragma unroll
-                for (int cs = 0; cs <= t / 2; ++cs) mma(acc, pa[lower_frag(t, cs)], ef[cs]);
-                O[t] += acc * (gpp[t] * fe.down);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int row = 16 * t + 4 * g + r;
-                    if (on && row < n) o[(ci * C + row) * o_step] = from_f32<In>(O[t][r]);
-                }
+                for (int cs = 0; cs <= t / 2; ++cs) mma(O[t], pa[lower_frag(t, cs)], ef[cs]);
+                O[t] *= down;
             }
-            fetch(pa, ws.PA + pbase(next), lane);
+            if (on) store_column(o + ci * C * step, oc, O, part.len - ci * C, g);
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (kAhead) fetch_p(next);
         }
-        m = 0.0f;
+        if constexpr (!kAhead) fetch_k(next);
+        // S = e^{G_C} S + K^T U, U = beta e^{G_C - G} E
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            E[t] *= gu[t];
-            m = largest(m, E[t]);
+        for (int t = 0; t < NT; ++t) E[t] *= gu[t];
+        m = largest_of(E);
+        if (Scale::over(m)) {
+            const float f = Scale::factor(m);
+            times(E, f);
+            times(S, f);
+            s.up *= f;
         }
-        fu(m);
         Frag<NS> uf[CS];
 #pragma unroll
-        for (int cs = 0; cs < CS; ++cs) split<NS>(E[2 * cs], E[2 * cs + 1], fu.up, uf[cs]);
+        for (int cs = 0; cs < CS; ++cs) split<NS>(E[2 * cs], E[2 * cs + 1], 1.0f, uf[cs]);
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
-            f32x4 acc = {};
+            S[i] *= last;
 #pragma unroll
-            for (int cs = 0; cs < CS; ++cs) mma(acc, kt[i * CS + cs], uf[cs]);
-            S[i] = S[i] * last + acc * fu.down;
+            for (int cs = 0; cs < CS; ++cs) mma(S[i], kt[i * CS + cs], uf[cs]);
         }
-        fetch(kt, ws.KT + kbase(next), lane);
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (kAhead) fetch_s(next);
+        if (Scale::under(most)) {
+            const float f = Scale::factor(most);
+            times(S, f);
+            s.up *= f;
+        }
     }
-    if (hT && on) {
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int row = 16 * m + 4 * g + r;
-                if (row < z.dk) hT[state + row * z.dv] = S[m][r];
-            }
-    }
-}
-
-// The same columns' state gradients from the last chunk to the first.
-template <typename In, int DK>
-__global__ __launch_bounds__(64, 1) void k_delta_walk_back(const Sizes z, const void* dop,
-                                                           const float* d_hT, void* dvp,
-                                                           float* d_h0, const Streams ws) {
-    constexpr int C = kChunk, NX = Planes<In>::kInput, NS = kPlanes;
-    constexpr int NT = C / 16, KS = DK / 32, CS = C / 32, MT = DK / 16;
-    const int lane = threadIdx.x % 64, g = lane / 16;
-    const int64_t seq = blockIdx.x;
-    const int h = blockIdx.y, hk = h / z.group;
-    const int col = blockIdx.z * 16 + lane % 16;
-    const bool on = col < z.dv;
-    const Span span = span_of(z, seq);
-    const int64_t state = (seq * z.heads_v + h) * z.dk * z.dv + col;
-    f32x4 S[MT];
+    const float down = 1.0f / s.up;
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int row = 16 * m + 4 * g + r;
-            S[m][r] = d_hT && on && row < z.dk ? d_hT[state + row * z.dv] : 0.0f;
+            const float x = S[m][r] * down;
+            if constexpr (kKind == kLocal) {
+                if (!blind) ws.segN[(unit * DK + row) * z.dvp + col] = x;
+                else ws.segM[(unit * DK + row) * DK + col - z.dvp] = x;
+            } else if (kKind == kOut && hT && part.last && on && row < z.dk) {
+                hT[state + row * z.dv] = x;
+            }
         }
+}
+
+// The same columns' state gradients from the last chunk to the first. kIsLocal:
+// a segment's, from a zero end.
+template <typename In, int DK, bool kIsLocal>
+__global__ __launch_bounds__(64, 1) void k_delta_walk_back(const Sizes z, const Segments sg,
+                                                            const void* dop, const float* d_hT,
+                                                            void* dvp, float* d_h0,
+                                                            const Streams ws) {
+    constexpr int C = kChunk, NX = Planes<In>::kInput, NS = kPlanes;
+    constexpr int NT = C / 16, KS = DK / 32, CS = C / 32, MT = DK / 16;
+    constexpr bool kAhead = DK * NX <= 64;  // as in the forward walk
+    Part part;
+    if (!part_of(z, sg, part) || (kIsLocal && part.first)) return;
+    const int lane = threadIdx.x, g = lane / 16;
+    const int ct = blockIdx.z;
+    const int h = blockIdx.y, hk = h / z.group;
+    const int col = ct * 16 + lane % 16;
+    const bool on = col < z.dv;
     const int64_t step = static_cast<int64_t>(z.heads_v) * z.dv;
-    const int64_t first = (span.start * z.heads_v + h) * z.dv;
-    const In* dO = static_cast<const In*>(dop) + first + (on ? col : 0);
-    In* dV = static_cast<In*>(dvp) + first + col;
-    const int64_t chunks = (span.len + C - 1) / C;
+    const int64_t unit = part.unit * z.heads_v + h;
+    const int64_t state = (part.seq * z.heads_v + h) * z.dk * z.dv + col;
+    const uint32_t tile_at = static_cast<uint32_t>(4 * g * z.dvp + col) * 4;
+
+    f32x4 S[MT];  // times scale.up, like all that follows
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int row = 16 * m + 4 * g + r;
+            float x = 0.0f;
+            if (!kIsLocal) {
+                if (!part.last) x = ws.segD[(unit * DK + row) * z.dvp + col];
+                else if (d_hT && on && row < z.dk) x = d_hT[state + row * z.dv];
+            }
+            S[m][r] = x;
+        }
+    const int64_t first = part.start * step + static_cast<int64_t>(h) * z.dv;
+    const In* dO = static_cast<const In*>(dop) + first;
+    In* dV = static_cast<In*>(dvp) + first;
+    const Column oc(static_cast<uint32_t>(step), g, on ? col : 0, sizeof(In));
 
     Frag<NX> ka[NT * KS], kt[MT * CS], qt[MT * CS];
     Frag<NS> pa[kTri], tt[kTri];
-    In yr[NT][4];
-    auto kbase = [&](int64_t ci) { return ((span.slot0 + ci) * z.heads_k + hk) * C * DK * NX; };
-    auto pbase = [&](int64_t ci) { return ((span.slot0 + ci) * z.heads_v + h) * kTriSize * NS; };
+    In yr[NT][4] = {};
+    f32x4 egk[NT], egq[NT], gu[NT];
+    float last = 0.0f, psc = 0.0f, tsc = 0.0f;
+    auto kbase = [&](int64_t ci) { return ((part.slot0 + ci) * z.heads_k + hk) * C * DK * NX; };
+    auto vslot = [&](int64_t ci) { return (part.slot0 + ci) * z.heads_v + h; };
+    auto gate = [&](int64_t ci, int which, f32x4 (&x)[NT]) {
+        const char* p = reinterpret_cast<const char*>(ws.gates + (vslot(ci) * kGates + which) * C);
+        const uint32_t at = static_cast<uint32_t>(g) * 16;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) x[t] = *reinterpret_cast<const f32x4*>(p + 64 * t + at);
+    };
     auto fetch_y = [&](int64_t ci) {
+        load_column(yr, dO + ci * C * step, oc, part.len - ci * C, g);
+    };
+    auto fetch_x = [&](int64_t ci) {
+        fetch(ka, ws.KA + kbase(ci), lane);
+        fetch(pa, ws.PA + vslot(ci) * kTriSize * NS, lane);
+        gate(ci, kU, gu);
+        gate(ci, kEgQ, egq);
+        psc = ws.gates[(vslot(ci) * kGates + kP) * C];
+    };
+    auto fetch_t = [&](int64_t ci) {
+        fetch(tt, ws.TT + vslot(ci) * kTriSize * NS, lane);
+        gate(ci, kEgK, egk);
+        tsc = ws.gates[(vslot(ci) * kGates + kT) * C];
+    };
+    auto fetch_s = [&](int64_t ci) {
+        fetch(qt, ws.QT + kbase(ci), lane);
+        fetch(kt, ws.KT + kbase(ci), lane);
+        last = ws.gates[(vslot(ci) * kGates + kEg) * C + C - 1];
+    };
+    if (part.c0 < part.c1) {
+        const int64_t ci = part.c1 - 1;
+        fetch_y(ci);
+        fetch_x(ci);
+        if constexpr (kAhead) {
+            fetch_t(ci);
+            fetch_s(ci);
+        }
+    }
+    Scale s;
+    {
+        float m = largest_of(S);
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                int64_t row = ci * C + 16 * t + 4 * g + r;
-                row = row < span.len ? row : span.len - 1;  // masked where it is used
-                yr[t][r] = dO[row * step];
-            }
-    };
-    if (chunks > 0) {
-        const int64_t ci = chunks - 1;
-        fetch_y(ci);
-        fetch(ka, ws.KA + kbase(ci), lane);
-        fetch(pa, ws.PA + pbase(ci), lane);
-        fetch(tt, ws.TT + pbase(ci), lane);
-        fetch(qt, ws.QT + kbase(ci), lane);
-        fetch(kt, ws.KT + kbase(ci), lane);
+            for (int r = 0; r < 4; ++r) m = __builtin_fmaxf(m, __builtin_fabsf(to_f32(yr[t][r])));
+        s.up = Scale::factor(m);
+        times(S, s.up);
     }
-    Fit fs, fo, fx, fy, fz;
-    for (int64_t ci = chunks - 1; ci >= 0; --ci) {
-        const int64_t next = ci > 0 ? ci - 1 : 0;
-        const int n = static_cast<int>(span.len - ci * C < C ? span.len - ci * C : C);
-        const int64_t vslot = (span.slot0 + ci) * z.heads_v + h;
-        const float* gates = ws.gates + vslot * kGates * C;
-        f32x4 egk[NT], egq[NT], gt[NT], gpp[NT], gu[NT];
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            const float* p = gates + 16 * t + 4 * g;
-            egk[t] = *reinterpret_cast<const f32x4*>(p + kEgK * C);
-            egq[t] = *reinterpret_cast<const f32x4*>(p + kEgQ * C);
-            gt[t] = *reinterpret_cast<const f32x4*>(p + kT2 * C);
-            gpp[t] = *reinterpret_cast<const f32x4*>(p + kP * C);
-            gu[t] = *reinterpret_cast<const f32x4*>(p + kU * C);
-        }
-        const float last = gates[kEg * C + C - 1];
-        float* ds = ws.dS + vslot * z.dk * z.dv + col;
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int row = 16 * m + 4 * g + r;
-                if (on && row < z.dk) ds[row * z.dv] = S[m][r];
-            }
+    for (int64_t ci = part.c1 - 1; ci >= part.c0; --ci) {
+        const int64_t next = ci > part.c0 ? ci - 1 : ci;
         f32x4 y[NT];
-        float m = 0.0f;
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                y[t][r] = on && 16 * t + 4 * g + r < n ? to_f32(yr[t][r]) : 0.0f;
-            m = largest(m, y[t]);
-        }
+            for (int r = 0; r < 4; ++r) y[t][r] = to_f32(yr[t][r]) * s.up;
+        __builtin_amdgcn_sched_barrier(0);
         fetch_y(next);
-        fo(m);
-        Frag<NX> dof[CS];
+        float m = __builtin_fmaxf(largest_of(S), largest_of(y)), most = m;
+        if (Scale::over(m)) {
+            const float f = Scale::factor(m);
+            times(S, f);
+            times(y, f);
+            s.up *= f;
+        }
+        if constexpr (!kIsLocal)
+            store_tiles(ws.dS + vslot(ci) * DK * z.dvp, tile_at, z.dvp, S, 1.0f / s.up);
+        if constexpr (!kAhead) fetch_t(ci);
+        // X = beta e^{G_C - G} K dS + (P diag(beta))^T dO
+        Frag<NX> yo[CS];
 #pragma unroll
-        for (int cs = 0; cs < CS; ++cs) split<NX>(y[2 * cs], y[2 * cs + 1], fo.up, dof[cs]);
-        m = 0.0f;
-#pragma unroll
-        for (int i = 0; i < MT; ++i) m = largest(m, S[i]);
-        fs(m);
+        for (int cs = 0; cs < CS; ++cs) split<NX>(y[2 * cs], y[2 * cs + 1], 1.0f, yo[cs]);
         Frag<NS> sf[KS];
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) split<NS>(S[2 * ks], S[2 * ks + 1], fs.up, sf[ks]);
+        for (int ks = 0; ks < KS; ++ks) split<NS>(S[2 * ks], S[2 * ks + 1], 1.0f, sf[ks]);
         f32x4 X[NT];
-        m = 0.0f;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             f32x4 a = {}, b = {};
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) mma(a, ka[t * KS + ks], sf[ks]);
 #pragma unroll
-            for (int cs = t / 2; cs < CS; ++cs) mma(b, pa[upper_frag(t, cs)], dof[cs]);
-            X[t] = a * (gu[t] * fs.down) + b * (gpp[t] * fo.down);
-            m = largest(m, X[t]);
+            for (int cs = t / 2; cs < CS; ++cs) mma(b, pa[upper_frag(t, cs)], yo[cs]);
+            X[t] = a * gu[t] + b * psc;
+            y[t] *= egq[t];
         }
-        fetch(ka, ws.KA + kbase(next), lane);
-        fetch(pa, ws.PA + pbase(next), lane);
-        fx(m);
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (kAhead) fetch_x(next);
+        else fetch_s(ci);
+        auto rescale = [&](f32x4 (&x)[NT], float top) {
+            const float f = Scale::factor(top);
+            times(x, f);
+            times(S, f);
+            times(y, f);
+            s.up *= f;
+        };
+        m = largest_of(X);
+        most = __builtin_fmaxf(most, m);
+        if (Scale::over(m)) rescale(X, m);
+        // dR = T^T X
         Frag<NS> xf[CS];
 #pragma unroll
-        for (int cs = 0; cs < CS; ++cs) split<NS>(X[2 * cs], X[2 * cs + 1], fx.up, xf[cs]);
-        float* dr = ws.dR + vslot * C * z.dv + col;
-        m = 0.0f;
-        float my = 0.0f;
+        for (int cs = 0; cs < CS; ++cs) split<NS>(X[2 * cs], X[2 * cs + 1], 1.0f, xf[cs]);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             X[t] = f32x4{};
 #pragma unroll
             for (int cs = t / 2; cs < CS; ++cs) mma(X[t], tt[upper_frag(t, cs)], xf[cs]);
-            X[t] *= gt[t] * fx.down;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int row = 16 * t + 4 * g + r;
-                if (on) dr[row * z.dv] = X[t][r];
-                if (on && row < n) dV[(ci * C + row) * step] = from_f32<In>(X[t][r]);
-            }
-            y[t] *= egq[t];
-            X[t] *= -egk[t];
-            my = largest(my, y[t]);
-            m = largest(m, X[t]);
         }
-        fetch(tt, ws.TT + pbase(next), lane);
-        fy(my);
-        fz(m);
+        if (tsc != 1.0f) times(X, tsc);
+        if constexpr (!kIsLocal) {
+            f32x4 d[NT];
+            const float down = 1.0f / s.up;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) d[t] = X[t] * down;
+            store_tiles(ws.dR + vslot(ci) * C * z.dvp, tile_at, z.dvp, d, 1.0f);
+            if (on) store_column(dV + ci * C * step, oc, d, part.len - ci * C, g);
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) X[t] *= -egk[t];
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (kAhead) fetch_t(next);
+        m = __builtin_fmaxf(largest_of(X), largest_of(y));
+        if (Scale::over(m)) rescale(X, m);
+        // dS = e^{G_C} dS + Q^T (scale e^G dO) - K^T (e^G dR)
         Frag<NS> yf[CS];
 #pragma unroll
         for (int cs = 0; cs < CS; ++cs) {
-            split<NS>(y[2 * cs], y[2 * cs + 1], fy.up, yf[cs]);
-            split<NS>(X[2 * cs], X[2 * cs + 1], fz.up, xf[cs]);
+            split<NS>(y[2 * cs], y[2 * cs + 1], 1.0f, yf[cs]);
+            split<NS>(X[2 * cs], X[2 * cs + 1], 1.0f, xf[cs]);
         }
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
-            f32x4 a = {}, b = {};
+            S[i] *= last;
 #pragma unroll
             for (int cs = 0; cs < CS; ++cs) {
-                mma(a, qt[i * CS + cs], yf[cs]);
-                mma(b, kt[i * CS + cs], xf[cs]);
+                mma(S[i], qt[i * CS + cs], yf[cs]);
+                mma(S[i], kt[i * CS + cs], xf[cs]);
             }
-            S[i] = S[i] * last + (a * fy.down + b * fz.down);
         }
-        fetch(qt, ws.QT + kbase(next), lane);
-        fetch(kt, ws.KT + kbase(next), lane);
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (kAhead) fetch_s(next);
+        else fetch_x(next);
+        if (Scale::under(most)) {
+            const float f = Scale::factor(most);
+            times(S, f);
+            s.up *= f;
+        }
     }
-    if (d_h0 && on) {
+    const float down = 1.0f / s.up;
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+    for (int m = 0; m < MT; ++m)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int row = 16 * m + 4 * g + r;
-                if (row < z.dk) d_h0[state + row * z.dv] = S[m][r];
+        for (int r = 0; r < 4; ++r) {
+            const int row = 16 * m + 4 * g + r;
+            if constexpr (kIsLocal) {
+                ws.segN[(unit * DK + row) * z.dvp + col] = S[m][r] * down;
+            } else if (d_h0 && part.first && on && row < z.dk) {
+                d_h0[state + row * z.dv] = S[m][r] * down;
             }
+        }
+}
+
+// Half h of a fragment in LDS, from four rows of a result tile.
+template <int N>
+__device__ __forceinline__ void publish(_Float16* frag, int h, int lane, f32x4 v, float up) {
+    f16x4 p[N];
+    split4<N>(v, up, p);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        *reinterpret_cast<f16x4*>(frag + i * 512 + lane * 8 + 4 * h) = p[i];
+}
+
+// States at the segments' starts from their local results, S <- M S + N segment
+// by segment (backward: gradients at their ends, dS <- M^T dS + N from the
+// last). One workgroup to 16 columns of a head, a wave to each 16 rows; each
+// result tile is published in LDS as half of an operand fragment for the next
+// product.
+template <int DK, bool kBack>
+__global__ __launch_bounds__(DK * 4) void k_delta_join(const Sizes z, const Segments sg,
+                                                       const float* ends, const Streams ws) {
+    constexpr int KS = DK / 32, MT = DK / 16, NS = kPlanes;
+    __shared__ __align__(16) _Float16 bS[2][KS * NS * 512];
+    __shared__ float most[2][2][MT];
+    const int lane = threadIdx.x % 64, w = threadIdx.x / 64, g = lane / 16, i = lane % 16;
+    const int64_t seq = blockIdx.x;
+    const int h = blockIdx.y, col = blockIdx.z * 16 + i;
+    const Span span = span_of(z, seq);
+    const int64_t chunks = (span.len + kChunk - 1) / kChunk;
+    const int64_t segs = (chunks + sg.chunks - 1) / sg.chunks;
+    const int64_t unit0 = span.slot0 / sg.chunks + seq;
+    const int row0 = 16 * w + 4 * g;
+    f32x4 S;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int row = row0 + r;
+        S[r] = ends && col < z.dv && row < z.dk
+                   ? ends[((seq * z.heads_v + h) * z.dk + row) * z.dv + col] : 0.0f;
+    }
+    auto fetch = [&](int64_t s, f32x4 (&m)[2 * KS], f32x4& add) {
+        const int64_t unit = (unit0 + s) * z.heads_v + h;
+        const float* M = ws.segM + unit * DK * DK;
+#pragma unroll
+        for (int k = 0; k < 2 * KS; ++k) {
+            if constexpr (kBack) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) m[k][r] = M[(16 * k + 4 * g + r) * DK + 16 * w + i];
+            } else {
+                m[k] = *reinterpret_cast<const f32x4*>(M + (16 * w + i) * DK + 16 * k + 4 * g);
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) add[r] = ws.segN[(unit * DK + row0 + r) * z.dvp + col];
+    };
+    f32x4 m[2 * KS], add;
+    const int64_t count = segs - 1;  // joints
+    auto seg = [&](int64_t k) { return kBack ? segs - 1 - k : k; };
+    if (count > 0) fetch(seg(0), m, add);
+    for (int64_t k = 0; k < count; ++k) {
+        const int par = static_cast<int>(k & 1);
+        // both operands scaled to their largest value
+        float ms = over_wave(largest(0.0f, S)), mm = 0.0f;
+#pragma unroll
+        for (int q = 0; q < 2 * KS; ++q) mm = largest(mm, m[q]);
+        mm = over_wave(mm);
+        if (lane == 0) most[par][0][w] = ms;
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < MT; ++q) ms = __builtin_fmaxf(ms, most[par][0][q]);
+        const float us = fitting(ms), um = fitting(mm);
+        publish<NS>(bS[par] + (w / 2) * NS * 512, w % 2, lane, S, us);
+        Frag<NS> a[KS];
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) split<NS>(m[2 * ks], m[2 * ks + 1], um, a[ks]);
+        const f32x4 plus = add;
+        if (k + 1 < count) fetch(seg(k + 1), m, add);
+        __syncthreads();
+        f32x4 acc = {};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) mma(acc, a[ks], load_frag<NS>(bS[par], ks, lane));
+        S = acc * ((1.0f / us) * (1.0f / um)) + plus;
+        // the start of the next segment, or the end of the one before
+        float* to = kBack ? ws.segD : ws.segS;
+        const int64_t unit = (unit0 + seg(k) + (kBack ? -1 : 1)) * z.heads_v + h;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) to[(unit * DK + row0 + r) * z.dvp + col] = S[r];
     }
 }
 
@@ -755,10 +1117,10 @@ __global__ __launch_bounds__(256) void k_delta_grads(const Sizes z, const void* 
     for (int h = hk * z.group; h < (hk + 1) * z.group; ++h) {
         const int64_t vslot = slot * z.heads_v + h;
         const float* gates = ws.gates + vslot * kGates * C;
-        const float* S0 = ws.S0 + vslot * z.dk * z.dv;
-        const float* dS = ws.dS + vslot * z.dk * z.dv;
-        const float* E = ws.E + vslot * C * z.dv;
-        const float* dR = ws.dR + vslot * C * z.dv;
+        const float* S0 = ws.S0 + vslot * DK * z.dvp;
+        const float* dS = ws.dS + vslot * DK * z.dvp;
+        const float* E = ws.E + vslot * C * z.dvp;
+        const float* dR = ws.dR + vslot * C * z.dvp;
         const In* dO = static_cast<const In*>(dop) + (c.token * z.heads_v + h) * z.dv;
         const int64_t o_step = static_cast<int64_t>(z.heads_v) * z.dv;
         const float eg = gates[kEg * C + tok], beta = gates[kBeta * C + tok];
@@ -779,8 +1141,8 @@ __global__ __launch_bounds__(256) void k_delta_grads(const Sizes z, const void* 
                 const int row = lrow + 16 * i;
                 re[i] = rr[i] = ro[i] = f32x4{};
                 if (in) {
-                    re[i] = load4(E + row * z.dv + at);
-                    rr[i] = load4(dR + row * z.dv + at);
+                    re[i] = load4(E + row * z.dvp + at);
+                    rr[i] = load4(dR + row * z.dvp + at);
                     if (row < c.n) ro[i] = load4(dO + row * o_step + at);
                 }
             }
@@ -789,8 +1151,8 @@ __global__ __launch_bounds__(256) void k_delta_grads(const Sizes z, const void* 
                 const int row = lrow + 16 * i;
                 rs[i] = rd[i] = f32x4{};
                 if (in && row < z.dk) {
-                    rs[i] = load4(S0 + static_cast<int64_t>(row) * z.dv + at);
-                    rd[i] = load4(dS + static_cast<int64_t>(row) * z.dv + at);
+                    rs[i] = load4(S0 + row * z.dvp + at);
+                    rd[i] = load4(dS + row * z.dvp + at);
                 }
             }
 #pragma unroll
@@ -933,7 +1295,7 @@ __global__ __launch_bounds__(256) void k_delta_grads(const Sizes z, const void* 
                 const float kkv = kk[r] * (gk[r] * kw_);
                 float cu = 0.0f, cl = 0.0f, f = 0.0f;
                 if (t <= w && row <= tok) {  // j = row, i = tok
-                    const float d = expf((ghi - hi[r]) + (glo - lo[r]));
+                    const float d = fast_exp2((ghi - hi[r]) + (glo - lo[r]));
                     const float db_j = d * bt[r];
                     cu = z.scale * db_j * np_up[t][r];
                     if (row < tok) {  // D_ii = 1 does not hang on G
@@ -942,7 +1304,7 @@ __global__ __launch_bounds__(256) void k_delta_grads(const Sizes z, const void* 
                     }
                 }
                 if (t >= w && row >= tok) {  // i = row, j = tok
-                    const float d = expf((hi[r] - ghi) + (lo[r] - glo));
+                    const float d = fast_exp2((hi[r] - ghi) + (lo[r] - glo));
                     const float pn = z.scale * d * (qk_low[r] * (gq[r] * kw_)) * np_low[t][r];
                     cl = z.scale * d * beta * np_low[t][r];
                     float mn = 0.0f;

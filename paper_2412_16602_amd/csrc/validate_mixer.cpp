@@ -12,6 +12,7 @@ namespace {
 
 constexpr int64_t kMaxRow = (int64_t{1} << 31) - 1;
 constexpr int64_t kMaxTotal = int64_t{1} << 40;
+constexpr int64_t kMaxToken = int64_t{1} << 22;  // delta rule: elements from token to token
 
 bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 bool valid_dtype(vmb_dtype t) { return t == VMB_F32 || t == VMB_BF16; }
@@ -62,6 +63,7 @@ vmb_status delta_sizes(int64_t batch, int64_t L, int64_t heads_k, int64_t heads_
                        int64_t dv) {
     if (batch < 1 || L < 1 || heads_k < 1 || heads_v < 1 || dk < 1 || dv < 1) return VMB_ERR_SHAPE;
     if (L > kMaxRow || heads_v % heads_k != 0 || heads_v > 65535) return VMB_ERR_SHAPE;
+    if (heads_v * dv > kMaxToken || heads_k * dk > kMaxToken) return VMB_ERR_SHAPE;
     if (prod({batch, L, heads_v}) < 0 || prod({batch, heads_v, dk, dv}) < 0) return VMB_ERR_SHAPE;
     if (dk % 8 != 0 || dv % 8 != 0 || dk > 128 || dv > 256) return VMB_ERR_UNSUPPORTED;
     return VMB_OK;
@@ -88,6 +90,8 @@ vmb_status validate_delta(const DeltaArgs& a, bool backward) {
     const int64_t ng = prod({a.batch, a.L, a.heads_v});
     if (nq < 0 || nk < 0 || nv < 0 || no < 0 || nqo < 0 || ns < 0 || ng < 0) return VMB_ERR_SHAPE;
     if (a.q_stride * e % 16 || a.k_stride * e % 16 || a.v_stride * e % 16) return VMB_ERR_SHAPE;
+    if (a.q_stride > kMaxToken || a.k_stride > kMaxToken || a.v_stride > kMaxToken)
+        return VMB_ERR_SHAPE;
     for (const void* p : {a.q, a.k, a.v, static_cast<const void*>(a.o), a.d_o,
                           static_cast<const void*>(a.d_q), static_cast<const void*>(a.d_k),
                           static_cast<const void*>(a.d_v), static_cast<const void*>(a.h0),
@@ -134,6 +138,8 @@ vmb_status validate_delta_step(const DeltaStepArgs& a) {
     const int64_t ng = prod({a.batch, a.T, a.heads_v});
     if (nq < 0 || nk < 0 || nv < 0 || no < 0 || ns < 0 || ng < 0) return VMB_ERR_SHAPE;
     if (a.q_stride * e % 16 || a.k_stride * e % 16 || a.v_stride * e % 16) return VMB_ERR_SHAPE;
+    if (a.q_stride > kMaxToken || a.k_stride > kMaxToken || a.v_stride > kMaxToken)
+        return VMB_ERR_SHAPE;
     for (const void* p : {a.q, a.k, a.v, static_cast<const void*>(a.o),
                           static_cast<const void*>(a.state)})
         if (!aligned(p, 16)) return VMB_ERR_ALIGN;
