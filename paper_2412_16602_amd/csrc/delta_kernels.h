@@ -485,18 +485,23 @@ __device__ __forceinline__ void times(f32x4 (&x)[TILES], float f) {
 }
 
 // The scale of a wave's operands, state included: everything the wave holds is
-// `up` times its value. Kept while the largest value of a chunk stays in
-// [2^5, 2^15), which ballots tell; values down to 2^-8 of it keep 22 bits,
-// smaller ones an error of 2^-30 of it.
+// `up` times its value. Kept while no operand reaches 2^15 and the largest
+// value of what goes on to the next chunk reaches 2^5, which ballots tell;
+// values down to 2^-8 of that keep 22 bits, smaller ones an error of 2^-30 of it.
 struct Scale {
     float up = 1.0f;
     // Whether m, a lane's largest value, is too large for half precision.
     __device__ __forceinline__ static bool over(float m) { return __ballot(!(m < 32768.0f)) != 0; }
-    // The factor that brings the wave's largest value into [2^9, 2^10).
-    __device__ __forceinline__ static float factor(float m) {
-        return fitting(over_wave(m)) * 0x1p-4f;
+    // Sets up so that the wave's largest value comes into [2^9, 2^10), within
+    // 2^-100 to 2^100 (a state that decays to nothing would take it to inf);
+    // returns the factor for what is held.
+    __device__ __forceinline__ float fit(float m) {
+        const float old = up;
+        up = __builtin_fminf(__builtin_fmaxf(old * fitting(over_wave(m)) * 0x1p-4f, 0x1p-100f),
+                             0x1p100f);
+        return up / old;
     }
-    // A chunk's largest value: too small, and not all zeros.
+    // Whether the largest value is too small, and not zero.
     __device__ __forceinline__ static bool under(float m) {
         return __ballot(m >= 32.0f) == 0 && __ballot(m > 0.0f) != 0;
     }
@@ -615,16 +620,14 @@ __global__ __launch_bounds__(64, 1) void k_delta_walk(const Sizes z, const Segme
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r) m = __builtin_fmaxf(m, __builtin_fabsf(to_f32(vr[t][r])));
-        s.up = Scale::factor(m);
-        times(S, s.up);
+        times(S, s.fit(m));
     }
     for (int64_t ci = part.c0; ci < part.c1; ++ci) {
         const int64_t next = ci + 1 < part.c1 ? ci + 1 : ci;
-        float m = largest_of(S), most = m;
+        float m = largest_of(S);
         if (Scale::over(m)) {
-            const float f = Scale::factor(m);
+            const float f = s.fit(m);
             times(S, f);
-            s.up *= f;
         }
         if constexpr (kKind == kSave)
             store_tiles(ws.S0 + vslot(ci) * DK * z.dvp, tile_at, z.dvp, S, 1.0f / s.up);
@@ -663,13 +666,11 @@ __global__ __launch_bounds__(64, 1) void k_delta_walk(const Sizes z, const Segme
         }
         if constexpr (!kAhead) fetch_s(ci);
         m = largest_of(R);
-        most = __builtin_fmaxf(most, m);
         auto rescale = [&](f32x4 (&x)[NT], float top) {  // the rest of what is held with it
-            const float f = Scale::factor(top);
+            const float f = s.fit(top);
             times(x, f);
             times(S, f);
             if constexpr (kKind == kOut) times(O, f);
-            s.up *= f;
         };
         if (Scale::over(m)) rescale(R, m);
         // E = T R
@@ -687,7 +688,6 @@ __global__ __launch_bounds__(64, 1) void k_delta_walk(const Sizes z, const Segme
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (kAhead) fetch_t(next);
         m = largest_of(E);
-        most = __builtin_fmaxf(most, m);
         if (Scale::over(m)) rescale(E, m);
         if constexpr (kKind == kSave)
             store_tiles(ws.E + vslot(ci) * C * z.dvp, tile_at, z.dvp, E, 1.0f / s.up);
@@ -711,29 +711,22 @@ __global__ __launch_bounds__(64, 1) void k_delta_walk(const Sizes z, const Segme
         // S = e^{G_C} S + K^T U, U = beta e^{G_C - G} E
 #pragma unroll
         for (int t = 0; t < NT; ++t) E[t] *= gu[t];
-        m = largest_of(E);
-        if (Scale::over(m)) {
-            const float f = Scale::factor(m);
+        times(S, last);
+        m = __builtin_fmaxf(largest_of(E), largest_of(S));  // all that goes on
+        if (Scale::over(m) || Scale::under(m)) {
+            const float f = s.fit(m);
             times(E, f);
             times(S, f);
-            s.up *= f;
         }
         Frag<NS> uf[CS];
 #pragma unroll
         for (int cs = 0; cs < CS; ++cs) split<NS>(E[2 * cs], E[2 * cs + 1], 1.0f, uf[cs]);
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            S[i] *= last;
+        for (int i = 0; i < MT; ++i)
 #pragma unroll
             for (int cs = 0; cs < CS; ++cs) mma(S[i], kt[i * CS + cs], uf[cs]);
-        }
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (kAhead) fetch_s(next);
-        if (Scale::under(most)) {
-            const float f = Scale::factor(most);
-            times(S, f);
-            s.up *= f;
-        }
     }
     const float down = 1.0f / s.up;
 #pragma unroll
@@ -840,8 +833,7 @@ __global__ __launch_bounds__(64, 1) void k_delta_walk_back(const Sizes z, const 
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r) m = __builtin_fmaxf(m, __builtin_fabsf(to_f32(yr[t][r])));
-        s.up = Scale::factor(m);
-        times(S, s.up);
+        times(S, s.fit(m));
     }
     for (int64_t ci = part.c1 - 1; ci >= part.c0; --ci) {
         const int64_t next = ci > part.c0 ? ci - 1 : ci;
@@ -852,12 +844,11 @@ __global__ __launch_bounds__(64, 1) void k_delta_walk_back(const Sizes z, const 
             for (int r = 0; r < 4; ++r) y[t][r] = to_f32(yr[t][r]) * s.up;
         __builtin_amdgcn_sched_barrier(0);
         fetch_y(next);
-        float m = __builtin_fmaxf(largest_of(S), largest_of(y)), most = m;
+        float m = __builtin_fmaxf(largest_of(S), largest_of(y));
         if (Scale::over(m)) {
-            const float f = Scale::factor(m);
+            const float f = s.fit(m);
             times(S, f);
             times(y, f);
-            s.up *= f;
         }
         if constexpr (!kIsLocal)
             store_tiles(ws.dS + vslot(ci) * DK * z.dvp, tile_at, z.dvp, S, 1.0f / s.up);
@@ -884,14 +875,12 @@ __global__ __launch_bounds__(64, 1) void k_delta_walk_back(const Sizes z, const 
         if constexpr (kAhead) fetch_x(next);
         else fetch_s(ci);
         auto rescale = [&](f32x4 (&x)[NT], float top) {
-            const float f = Scale::factor(top);
+            const float f = s.fit(top);
             times(x, f);
             times(S, f);
             times(y, f);
-            s.up *= f;
         };
         m = largest_of(X);
-        most = __builtin_fmaxf(most, m);
         if (Scale::over(m)) rescale(X, m);
         // dR = T^T X
         Frag<NS> xf[CS];
@@ -916,8 +905,9 @@ __global__ __launch_bounds__(64, 1) void k_delta_walk_back(const Sizes z, const 
         for (int t = 0; t < NT; ++t) X[t] *= -egk[t];
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (kAhead) fetch_t(next);
-        m = __builtin_fmaxf(largest_of(X), largest_of(y));
-        if (Scale::over(m)) rescale(X, m);
+        times(S, last);
+        m = __builtin_fmaxf(__builtin_fmaxf(largest_of(X), largest_of(y)), largest_of(S));
+        if (Scale::over(m) || Scale::under(m)) rescale(X, m);
         // dS = e^{G_C} dS + Q^T (scale e^G dO) - K^T (e^G dR)
         Frag<NS> yf[CS];
 #pragma unroll
@@ -927,7 +917,6 @@ __global__ __launch_bounds__(64, 1) void k_delta_walk_back(const Sizes z, const 
         }
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
-            S[i] *= last;
 #pragma unroll
             for (int cs = 0; cs < CS; ++cs) {
                 mma(S[i], qt[i * CS + cs], yf[cs]);
@@ -937,11 +926,6 @@ __global__ __launch_bounds__(64, 1) void k_delta_walk_back(const Sizes z, const 
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (kAhead) fetch_s(next);
         else fetch_x(next);
-        if (Scale::under(most)) {
-            const float f = Scale::factor(most);
-            times(S, f);
-            s.up *= f;
-        }
     }
     const float down = 1.0f / s.up;
 #pragma unroll

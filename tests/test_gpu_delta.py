@@ -155,6 +155,66 @@ def test_gates_at_their_ends(dtype):
     assert not got[3][:, [40, 100, 101], 0].any()
 
 
+@pytest.mark.parametrize("decay", ["slow", "fast", "gone"])
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(1, 4200, 1, 2, 32, 48), (1, 4609, 1, 1, 64, 16),
+                                   (1, 4100, 1, 1, 128, 32)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_long_sequences_in_segments(shape, dtype, decay):
+    """Few heads and many chunks: the walk is split and joined again. Decays
+    that keep a state over segments, that end it within one, and that leave
+    nothing of it after a chunk."""
+    *x, h0 = make(*shape, dtype, seed=17)
+    x[3].mul_({"slow": 0.02, "fast": 1.0, "gone": 100.0}[decay])
+    o, hT = forward(x, h0)
+    ro, rS = delta_ref(*x, 0.125, h0)
+    check(o, ro, "o")
+    check(hT, rS, "hT")
+    if decay == "slow" or shape[1] == 4200:
+        g = torch.Generator().manual_seed(2)
+        do = torch.randn(x[2].shape, generator=g).to(dtype).cuda()
+        dhT = torch.randn(h0.shape, generator=g).cuda()
+        got = backward(x, do, h0, dhT)
+        ref = delta_ref(*x, 0.125, h0, do=do, dhT=dhT)
+        for name, a, b in zip(("dq", "dk", "dv", "dg", "dbeta", "dh0"), got, ref):
+            check(a, b, name)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_packed_long_and_short(dtype):
+    """Packed sequences of which one is split into segments."""
+    cu = [0, 1, 4300, 4300, 4400, 8700]
+    *x, h0 = make(1, cu[-1], 1, 1, 32, 32, dtype, seed=18, n=5)
+    x[3].mul_(0.05)
+    o, hT = forward(x, h0, cu)
+    ro, rS = delta_ref(*x, 0.125, h0, cu)
+    check(o, ro, "o")
+    check(hT, rS, "hT")
+    do = torch.randn(x[2].shape, generator=torch.Generator().manual_seed(1)).to(dtype).cuda()
+    got = backward(x, do, h0, h0, cu)
+    ref = delta_ref(*x, 0.125, h0, cu, do=do, dhT=h0)
+    for name, a, b in zip(("dq", "dk", "dv", "dg", "dbeta", "dh0"), got, ref):
+        check(a, b, name)
+
+
+@pytest.mark.parametrize("size", [1e-12, 1e12])
+def test_values_of_any_size(size):
+    """Values and gradients far from 1, and one that is far from the rest."""
+    *x, h0 = make(1, 300, 1, 1, 64, 32, F32, seed=19)
+    x[2].mul_(size)
+    x[2][0, 100, 0, 3] *= 1e4
+    h0.mul_(size)
+    do = size * torch.randn(x[2].shape, generator=torch.Generator().manual_seed(1)).cuda()
+    o, hT = forward(x, h0)
+    ro, rS = delta_ref(*x, 0.125, h0)
+    check(o, ro, "o")
+    check(hT, rS, "hT")
+    got = backward(x, do, h0)
+    ref = delta_ref(*x, 0.125, h0, do=do)
+    for name, a, b in zip(("dq", "dk", "dv", "dg", "dbeta", "dh0"), got, ref):
+        check(a, b, name)
+
+
 def test_keys_that_repeat():
     """All keys of a head equal and beta 1: the triangular matrix of a chunk
     is the worst conditioned one that unit keys give."""
