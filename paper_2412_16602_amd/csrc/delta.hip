@@ -149,7 +149,7 @@ void backward(const DeltaArgs& a, const Sizes& z, const Segments& sg, const Stre
     k_delta_walk_back<In, DK, false><<<grid, 64, 0, a.stream>>>(z, sg, a.d_o, a.d_hT, a.d_v,
                                                                 a.d_h0, ws);
     const dim3 keys(static_cast<unsigned>(z.slots), static_cast<unsigned>(z.heads_k));
-    k_delta_grads<In, DK><<<keys, 256, 0, a.stream>>>(z, a.q, a.k, a.d_o, a.d_q, a.d_k, a.g,
+    k_delta_grads<In, DK><<<keys, 256, 0, a.stream>>>(z, a.d_o, a.d_q, a.d_k, a.g,
                                                       a.h0 == nullptr, a.d_g, a.d_beta, ws);
 }
 

@@ -124,15 +124,43 @@ __device__ __forceinline__ float fitting(float m) {
     return __builtin_ldexpf(1.0f, e);
 }
 
-// Largest value over the four lanes that share lane % 16, or over the wave.
+// f of the values of lanes l and l ^ 16, and of l and l ^ 32, in all lanes: the
+// swaps exchange the odd rows of 16 lanes (the upper 32) of one copy with the
+// even rows (the lower 32) of another.
+template <typename F>
+__device__ __forceinline__ float groups(float v, F f) {
+    const unsigned x = __float_as_uint(v);
+    const auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    const unsigned y = __float_as_uint(f(__uint_as_float(a[0]), __uint_as_float(a[1])));
+    const auto b = __builtin_amdgcn_permlane32_swap(y, y, false, false);
+    return f(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+// f over the 16 lanes of a row, by rotations.
+template <int kBy>
+__device__ __forceinline__ float rotated(float v) {
+    return __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(v), 0x120 + kBy, 0xf, 0xf,
+                                                       false));
+}
+template <typename F>
+__device__ __forceinline__ float row16(float v, F f) {
+    v = f(v, rotated<8>(v));
+    v = f(v, rotated<4>(v));
+    v = f(v, rotated<2>(v));
+    return f(v, rotated<1>(v));
+}
+// Largest value over the four lanes that share lane % 16, or over the wave;
+// sums likewise, in a fixed order.
 __device__ __forceinline__ float over_groups(float m) {
-    m = __builtin_fmaxf(m, __shfl_xor(m, 16));
-    return __builtin_fmaxf(m, __shfl_xor(m, 32));
+    return groups(m, [](float a, float b) { return __builtin_fmaxf(a, b); });
 }
 __device__ __forceinline__ float over_wave(float m) {
-#pragma unroll
-    for (int s = 1; s < 64; s *= 2) m = __builtin_fmaxf(m, __shfl_xor(m, s));
-    return m;
+    return over_groups(row16(m, [](float a, float b) { return __builtin_fmaxf(a, b); }));
+}
+__device__ __forceinline__ float sum_groups(float m) {
+    return groups(m, [](float a, float b) { return a + b; });
+}
+__device__ __forceinline__ float sum_wave(float m) {
+    return sum_groups(row16(m, [](float a, float b) { return a + b; }));
 }
 
 // The accumulator of a 16 x 16 tile: lane l holds column l % 16, rows
@@ -152,6 +180,14 @@ __device__ __forceinline__ f32x4 load4(const bf16_t* p) {
 }
 __device__ __forceinline__ f32x4 load4(const float* p) {
     return *reinterpret_cast<const f32x4*>(p);
+}
+__device__ __forceinline__ void store4(float* p, f32x4 v) { *reinterpret_cast<f32x4*>(p) = v; }
+__device__ __forceinline__ void store4(bf16_t* p, f32x4 v) {
+    typedef unsigned short u16x4 __attribute__((ext_vector_type(4)));
+    u16x4 x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = from_f32<bf16_t>(v[i]).bits;
+    *reinterpret_cast<u16x4*>(p) = x;
 }
 
 // Planes of an input operand: half precision holds a scaled bfloat16 value,

@@ -150,8 +150,8 @@ __global__ __launch_bounds__(256) void k_delta_prepare(const Sizes z, const void
         }
         const float uk = fitting(over_groups(mk)) * 0x1p-14f,  // largest in [1/2, 1)
                     uq = fitting(over_groups(mq)) * 0x1p-14f;
-        kcol = 1.0f / uk;
-        qcol = 1.0f / uq;
+        kcol = fast_rcp(uk);
+        qcol = fast_rcp(uq);
         if (g == 0) {
             sk[mine] = kcol;
             sq[mine] = qcol;
@@ -273,7 +273,7 @@ __global__ __launch_bounds__(256) void k_delta_prepare(const Sizes z, const void
             gates[kEgK * C + lane] = eg * k1;
             gates[kEgQ * C + lane] = z.scale * eg * q1 * (kBack ? 1.0f : up);
             gates[kU * C + lane] = sbeta[lane] * end * k1;
-            if (lane == 0) gates[kP * C] = 1.0f / up;
+            if (lane == 0) gates[kP * C] = fast_rcp(up);
         }
     }
 
@@ -365,7 +365,7 @@ __global__ __launch_bounds__(256) void k_delta_prepare(const Sizes z, const void
     // T's diagonal is 1: as it is, unless it does not fit half precision
     const float up = m < 32768.0f ? 1.0f : fitting(m);
     store_tri(ws.TA + pbase, v, up, true);
-    if (threadIdx.x == 0) gates[kT * C] = 1.0f / up;
+    if (threadIdx.x == 0) gates[kT * C] = fast_rcp(up);
     if constexpr (kBack) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
@@ -499,7 +499,7 @@ struct Scale {
         const float old = up;
         up = __builtin_fminf(__builtin_fmaxf(old * fitting(over_wave(m)) * 0x1p-4f, 0x1p-100f),
                              0x1p100f);
-        return up / old;
+        return up * fast_rcp(old);  // powers of two: exact
     }
     // Whether the largest value is too small, and not zero.
     __device__ __forceinline__ static bool under(float m) {
@@ -630,7 +630,7 @@ __global__ __launch_bounds__(64, 1) void k_delta_walk(const Sizes z, const Segme
             times(S, f);
         }
         if constexpr (kKind == kSave)
-            store_tiles(ws.S0 + vslot(ci) * DK * z.dvp, tile_at, z.dvp, S, 1.0f / s.up);
+            store_tiles(ws.S0 + vslot(ci) * DK * z.dvp, tile_at, z.dvp, S, on ? fast_rcp(s.up) : 0.0f);
         if constexpr (!kAhead) {
             fetch_t(ci);
             if constexpr (kKind == kOut) fetch_q(ci);
@@ -690,13 +690,13 @@ __global__ __launch_bounds__(64, 1) void k_delta_walk(const Sizes z, const Segme
         m = largest_of(E);
         if (Scale::over(m)) rescale(E, m);
         if constexpr (kKind == kSave)
-            store_tiles(ws.E + vslot(ci) * C * z.dvp, tile_at, z.dvp, E, 1.0f / s.up);
+            store_tiles(ws.E + vslot(ci) * C * z.dvp, tile_at, z.dvp, E, on ? fast_rcp(s.up) : 0.0f);
         // O = scale e^G Q S + P diag(beta) E
         if constexpr (kKind == kOut) {
             Frag<NS> ef[CS];
 #pragma unroll
             for (int cs = 0; cs < CS; ++cs) split<NS>(E[2 * cs], E[2 * cs + 1], 1.0f, ef[cs]);
-            const float down = psc / s.up;  // the gates of Q hold P's scale
+            const float down = psc * fast_rcp(s.up);  // the gates of Q hold P's scale
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
 #pragma unroll
@@ -728,7 +728,7 @@ __global__ __launch_bounds__(64, 1) void k_delta_walk(const Sizes z, const Segme
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (kAhead) fetch_s(next);
     }
-    const float down = 1.0f / s.up;
+    const float down = fast_rcp(s.up);
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -851,7 +851,8 @@ __global__ __launch_bounds__(64, 1) void k_delta_walk_back(const Sizes z, const 
             times(y, f);
         }
         if constexpr (!kIsLocal)
-            store_tiles(ws.dS + vslot(ci) * DK * z.dvp, tile_at, z.dvp, S, 1.0f / s.up);
+            store_tiles(ws.dS + vslot(ci) * DK * z.dvp, tile_at, z.dvp, S,
+                        on ? fast_rcp(s.up) : 0.0f);
         if constexpr (!kAhead) fetch_t(ci);
         // X = beta e^{G_C - G} K dS + (P diag(beta))^T dO
         Frag<NX> yo[CS];
@@ -895,10 +896,10 @@ __global__ __launch_bounds__(64, 1) void k_delta_walk_back(const Sizes z, const 
         if (tsc != 1.0f) times(X, tsc);
         if constexpr (!kIsLocal) {
             f32x4 d[NT];
-            const float down = 1.0f / s.up;
+            const float down = fast_rcp(s.up);
 #pragma unroll
             for (int t = 0; t < NT; ++t) d[t] = X[t] * down;
-            store_tiles(ws.dR + vslot(ci) * C * z.dvp, tile_at, z.dvp, d, 1.0f);
+            store_tiles(ws.dR + vslot(ci) * C * z.dvp, tile_at, z.dvp, d, on ? 1.0f : 0.0f);
             if (on) store_column(dV + ci * C * step, oc, d, part.len - ci * C, g);
         }
 #pragma unroll
@@ -927,7 +928,7 @@ __global__ __launch_bounds__(64, 1) void k_delta_walk_back(const Sizes z, const 
         if constexpr (kAhead) fetch_s(next);
         else fetch_x(next);
     }
-    const float down = 1.0f / s.up;
+    const float down = fast_rcp(s.up);
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -1018,7 +1019,7 @@ __global__ __launch_bounds__(DK * 4) void k_delta_join(const Sizes z, const Segm
         f32x4 acc = {};
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) mma(acc, a[ks], load_frag<NS>(bS[par], ks, lane));
-        S = acc * ((1.0f / us) * (1.0f / um)) + plus;
+        S = acc * (fast_rcp(us) * fast_rcp(um)) + plus;
         // the start of the next segment, or the end of the one before
         float* to = kBack ? ws.segD : ws.segS;
         const int64_t unit = (unit0 + seg(k) + (kBack ? -1 : 1)) * z.heads_v + h;
@@ -1058,25 +1059,36 @@ __device__ __forceinline__ Frag<N> lds_frag(const _Float16* base, int rows, int 
 template <int N>
 __device__ __forceinline__ void lds_put(_Float16* base, int rows, int row, int at, f32x4 v,
                                         float up) {
+    f16x4 h[N];
+    split4<N>(v, up, h);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] *= up;
+    for (int n = 0; n < N; ++n)
+        *reinterpret_cast<f16x4*>(base + (n * rows + row) * kPitch + at) = h[n];
+}
+
+// A pointer whose loads stay where they are written (they would be moved out of
+// the loops and held in registers).
+__device__ __forceinline__ const _Float16* here(const _Float16* p) {
+    asm volatile("" : "+s"(p));
+    return p;
+}
+
+// Four values of a fragment (half h) as binary32.
+template <int N>
+__device__ __forceinline__ f32x4 half_of(const Frag<N>& f, int h) {
+    f32x4 v;
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
-        f16x4 h;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            h[i] = static_cast<_Float16>(v[i]);
-            v[i] -= static_cast<float>(h[i]);
-        }
-        *reinterpret_cast<f16x4*>(base + (n * rows + row) * kPitch + at) = h;
+    for (int i = 0; i < 4; ++i) {
+        v[i] = static_cast<float>(f.p[0][4 * h + i]);
+        if constexpr (N > 1) v[i] += static_cast<float>(f.p[1][4 * h + i]);
     }
+    return v;
 }
 
 template <typename In, int DK>
-__global__ __launch_bounds__(256) void k_delta_grads(const Sizes z, const void* qp, const void* kp,
-                                                     const void* dop, void* dqp, void* dkp,
-                                                     const float* gp, bool from_zero, float* dgp,
-                                                     float* dbp, const Streams ws) {
+__global__ __launch_bounds__(256, DK * Planes<In>::kInput > 64 ? 1 : 2) void k_delta_grads(
+    const Sizes z, const void* dop, void* dqp, void* dkp, const float* gp, bool from_zero,
+    float* dgp, float* dbp, const Streams ws) {
     constexpr int C = kChunk, NX = Planes<In>::kInput, NS = kPlanes;
     constexpr int NT = C / 16, KS = DK / 32, CS = C / 32, MT = DK / 16, VS = kVB / 32;
     __shared__ __align__(16) _Float16 se[NS * C * kPitch], sr[NS * C * kPitch],
@@ -1086,76 +1098,64 @@ __global__ __launch_bounds__(256) void k_delta_grads(const Sizes z, const void* 
     const int hk = blockIdx.y;
     const Chunk c = chunk_of(z, slot);
     if (c.n == 0) return;
-    const int lane = threadIdx.x % 64, w = threadIdx.x / 64;
+    const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int col = lane % 16, g = lane / 16;
     const int tok = 16 * w + col;  // this lane's token of the chunk
-    const bool has = tok < c.n;
     const int64_t kbase = (slot * z.heads_k + hk) * C * DK * NX;
-    const In* qrow = static_cast<const In*>(qp) + (c.token + tok) * z.q_stride +
-                     static_cast<int64_t>(hk) * z.dk;
-    const In* krow = static_cast<const In*>(kp) + (c.token + tok) * z.k_stride +
-                     static_cast<int64_t>(hk) * z.dk;
     const int lrow = threadIdx.x / 16, lcol = threadIdx.x % 16 * 4;  // staging: rows 16 apart
     f32x4 dq[MT] = {}, dk[MT] = {};
 
     for (int h = hk * z.group; h < (hk + 1) * z.group; ++h) {
         const int64_t vslot = slot * z.heads_v + h;
         const float* gates = ws.gates + vslot * kGates * C;
-        const float* S0 = ws.S0 + vslot * DK * z.dvp;
-        const float* dS = ws.dS + vslot * DK * z.dvp;
-        const float* E = ws.E + vslot * C * z.dvp;
-        const float* dR = ws.dR + vslot * C * z.dvp;
-        const In* dO = static_cast<const In*>(dop) + (c.token * z.heads_v + h) * z.dv;
         const int64_t o_step = static_cast<int64_t>(z.heads_v) * z.dv;
+        const In* dO = static_cast<const In*>(dop) + c.token * o_step + static_cast<int64_t>(h) * z.dv;
         const float eg = gates[kEg * C + tok], beta = gates[kBeta * C + tok];
         const float eend = gates[kEnd * C + tok];
-        const float ghi = gates[kGhi * C + tok], glo = gates[kGlo * C + tok];
+        const float kscale = gates[kK * C + tok], qscale = gates[kQ * C + tok];
 
         // NP and N: [t] with rows in tile t, columns this wave's tokens.
         // up: rows j <= columns i (transposed); low: rows i >= columns j.
         f32x4 np_up[NT] = {}, n_up[NT] = {}, np_low[NT] = {}, n_low[NT] = {};
-        float dG = 0.0f, db = 0.0f, wi = 0.0f, dot = 0.0f;
+        float dG = 0.0f, db = 0.0f, dot = 0.0f;
         for (int v0 = 0; v0 < z.dv; v0 += kVB) {
             const int at = v0 + lcol;
-            const bool in = at < z.dv;
-            f32x4 re[NT], rr[NT], ro[NT], rs[MT], rd[MT];
-            float mx[5] = {};
+            const bool in = at < z.dvp;  // the workspace's columns past dv hold zeros
+            f32x4 re[NT] = {}, rr[NT] = {}, ro[NT] = {}, rs[MT] = {}, rd[MT] = {};
+            if (in) {
+                const float* E = ws.E + (vslot * C + lrow) * z.dvp + at;
+                const float* dR = ws.dR + (vslot * C + lrow) * z.dvp + at;
+                const float* S0 = ws.S0 + (vslot * DK + lrow) * z.dvp + at;
+                const float* dS = ws.dS + (vslot * DK + lrow) * z.dvp + at;
 #pragma unroll
-            for (int i = 0; i < NT; ++i) {
-                const int row = lrow + 16 * i;
-                re[i] = rr[i] = ro[i] = f32x4{};
-                if (in) {
-                    re[i] = load4(E + row * z.dvp + at);
-                    rr[i] = load4(dR + row * z.dvp + at);
-                    if (row < c.n) ro[i] = load4(dO + row * o_step + at);
+                for (int i = 0; i < NT; ++i) {
+                    re[i] = load4(E + 16 * i * z.dvp);
+                    rr[i] = load4(dR + 16 * i * z.dvp);
+                }
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    rs[i] = load4(S0 + 16 * i * z.dvp);
+                    rd[i] = load4(dS + 16 * i * z.dvp);
+                }
+            }
+            if (at < z.dv) {
+#pragma unroll
+                for (int i = 0; i < NT; ++i) {
+                    // rows behind the last token repeat it: their q is zero
+                    const int row = lrow + 16 * i < c.n ? lrow + 16 * i : c.n - 1;
+                    ro[i] = load4(dO + row * o_step + at);
                 }
             }
 #pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                const int row = lrow + 16 * i;
-                rs[i] = rd[i] = f32x4{};
-                if (in && row < z.dk) {
-                    rs[i] = load4(S0 + row * z.dvp + at);
-                    rd[i] = load4(dS + row * z.dvp + at);
-                }
-            }
+            for (int i = 0; i < MT; ++i)
 #pragma unroll
-            for (int i = 0; i < NT; ++i) {
-                mx[0] = largest(mx[0], re[i]);
-                mx[1] = largest(mx[1], rr[i]);
-                mx[2] = largest(mx[2], ro[i]);
-            }
-#pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                mx[3] = largest(mx[3], rs[i]);
-                mx[4] = largest(mx[4], rd[i]);
-                const f32x4 x = rs[i] * rd[i];
-                dot += (x[0] + x[1]) + (x[2] + x[3]);
-            }
+                for (int r = 0; r < 4; ++r) dot = __builtin_fmaf(rs[i][r], rd[i][r], dot);
+            const float mx[5] = {largest_of(re), largest_of(rr), largest_of(ro), largest_of(rs),
+                                 largest_of(rd)};
 #pragma unroll
             for (int a = 0; a < 5; ++a) {
-                mx[a] = over_wave(mx[a]);
-                if (lane == 0) smax[a][w] = mx[a];
+                const float x = over_wave(mx[a]);
+                if (lane == 0) smax[a][w] = x;
             }
             __syncthreads();
             float up[5], down[5];
@@ -1165,7 +1165,7 @@ __global__ __launch_bounds__(256) void k_delta_grads(const Sizes z, const void* 
 #pragma unroll
                 for (int i = 1; i < NT; ++i) m = __builtin_fmaxf(m, smax[a][i]);
                 up[a] = fitting(m);
-                down[a] = 1.0f / up[a];
+                down[a] = fast_rcp(up[a]);
             }
 #pragma unroll
             for (int i = 0; i < NT; ++i) {
@@ -1189,6 +1189,7 @@ __global__ __launch_bounds__(256) void k_delta_grads(const Sizes z, const void* 
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
                 const int row = 16 * t + col;
+                __builtin_amdgcn_sched_barrier(0);
                 if (t <= w) {
                     f32x4 a = {}, b = {};
 #pragma unroll
@@ -1211,10 +1212,14 @@ __global__ __launch_bounds__(256) void k_delta_grads(const Sizes z, const void* 
                     n_low[t] += b * er;
                 }
             }
-            // the parts through the states
+            // the parts through the states; a fragment of Q or K by rows holds a
+            // token's elements in the accumulators' order
             const float sy = z.scale * eg * (down[3] * down[2]), sv = eg * (down[3] * down[1]);
+            float gq = 0.0f, gk = 0.0f;
+            const _Float16 *KA = here(ws.KA + kbase), *QA = here(ws.QA + kbase);
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
+                if (m % 2 == 0) __builtin_amdgcn_sched_barrier(0);
                 f32x4 y = {}, r = {};
 #pragma unroll
                 for (int s = 0; s < VS; ++s) {
@@ -1226,46 +1231,54 @@ __global__ __launch_bounds__(256) void k_delta_grads(const Sizes z, const void* 
                 r *= sv;
                 dq[m] += y;
                 dk[m] -= r;
-                const int k0 = 16 * m + 4 * g;
-                if (has && k0 < z.dk) {
-                    const f32x4 x = load4(qrow + k0) * y - load4(krow + k0) * r;
-                    dG += (x[0] + x[1]) + (x[2] + x[3]);
+                const f32x4 qv = half_of(load_frag<NX>(QA, w * KS + m / 2, lane), m % 2);
+                const f32x4 kv = half_of(load_frag<NX>(KA, w * KS + m / 2, lane), m % 2);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    gq = __builtin_fmaf(qv[i], y[i], gq);
+                    gk = __builtin_fmaf(kv[i], r[i], gk);
                 }
             }
+            dG += gq * qscale - gk * kscale;
+            // the gradient of the state behind the chunk takes its entry state's place
             __syncthreads();
 #pragma unroll
             for (int i = 0; i < MT; ++i) lds_put<NS>(sst, DK, lrow + 16 * i, lcol, rd[i], up[4]);
             __syncthreads();
             const float sz = eend * (down[4] * down[0]);
+            float gz = 0.0f;
+            KA = here(KA);
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
+                if (m % 2 == 0) __builtin_amdgcn_sched_barrier(0);
                 f32x4 e = {};
 #pragma unroll
                 for (int s = 0; s < VS; ++s)
                     mma(e, lds_frag<NS>(sst, DK, 16 * m + col, s, g), be[s]);
                 e *= sz;
                 dk[m] += e * beta;
-                const int k0 = 16 * m + 4 * g;
-                if (has && k0 < z.dk) {
-                    const f32x4 x = load4(krow + k0) * e;
-                    db += (x[0] + x[1]) + (x[2] + x[3]);
-                }
+                const f32x4 kv = half_of(load_frag<NX>(KA, w * KS + m / 2, lane), m % 2);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) gz = __builtin_fmaf(kv[i], e[i], gz);
             }
+            db += gz * kscale;
         }
-        wi = db * beta;
+        float wi = db * beta;
 
-        const float kw_ = gates[kK * C + tok], qw_ = gates[kQ * C + tok];
+        const float ghi = gates[kGhi * C + tok], glo = gates[kGlo * C + tok];
         float mu = 0.0f, ml = 0.0f, mf = 0.0f;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
+            __builtin_amdgcn_sched_barrier(0);  // one tile's operands at a time
+            const _Float16 *KA = here(ws.KA + kbase), *QA = here(ws.QA + kbase);
             f32x4 qk_up = {}, kk = {}, qk_low = {};
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
-                const Frag<NX> kw = load_frag<NX>(ws.KA + kbase, w * KS + ks, lane);
-                const Frag<NX> kt = load_frag<NX>(ws.KA + kbase, t * KS + ks, lane);
+                const Frag<NX> kw = load_frag<NX>(KA, w * KS + ks, lane);
+                const Frag<NX> kt = load_frag<NX>(KA, t * KS + ks, lane);
                 mma(kk, kt, kw);
-                if (t <= w) mma(qk_up, kt, load_frag<NX>(ws.QA + kbase, w * KS + ks, lane));
-                if (t >= w) mma(qk_low, load_frag<NX>(ws.QA + kbase, t * KS + ks, lane), kw);
+                if (t <= w) mma(qk_up, kt, load_frag<NX>(QA, w * KS + ks, lane));
+                if (t >= w) mma(qk_low, load_frag<NX>(QA, t * KS + ks, lane), kw);
             }
             const float* p = gates + 16 * t + 4 * g;
             const f32x4 hi = *reinterpret_cast<const f32x4*>(p + kGhi * C);
@@ -1276,28 +1289,26 @@ __global__ __launch_bounds__(256) void k_delta_grads(const Sizes z, const void* 
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int row = 16 * t + 4 * g + r;
-                const float kkv = kk[r] * (gk[r] * kw_);
+                const float kkv = kk[r] * (gk[r] * kscale);
+                const float up = (ghi - hi[r]) + (glo - lo[r]);
                 float cu = 0.0f, cl = 0.0f, f = 0.0f;
-                if (t <= w && row <= tok) {  // j = row, i = tok
-                    const float d = fast_exp2((ghi - hi[r]) + (glo - lo[r]));
-                    const float db_j = d * bt[r];
-                    cu = z.scale * db_j * np_up[t][r];
-                    if (row < tok) {  // D_ii = 1 does not hang on G
-                        f = db_j * n_up[t][r];
-                        dG += cu * (qk_up[r] * (gk[r] * qw_)) - f * kkv;
-                    }
+                if (t <= w) {  // j = row, i = tok: rows above the diagonal, and on it
+                    const float d = row <= tok ? fast_exp2(up) * bt[r] : 0.0f;
+                    cu = z.scale * d * np_up[t][r];
+                    f = row < tok ? d * n_up[t][r] : 0.0f;
+                    // D_ii = 1 does not hang on G
+                    const float x = cu * (qk_up[r] * (gk[r] * qscale)) - f * kkv;
+                    dG += row < tok ? x : 0.0f;
                 }
-                if (t >= w && row >= tok) {  // i = row, j = tok
-                    const float d = fast_exp2((hi[r] - ghi) + (lo[r] - glo));
-                    const float pn = z.scale * d * (qk_low[r] * (gq[r] * kw_)) * np_low[t][r];
-                    cl = z.scale * d * beta * np_low[t][r];
-                    float mn = 0.0f;
-                    if (row > tok) {
-                        mn = d * kkv * n_low[t][r];
-                        f = d * beta * n_low[t][r];
-                    }
-                    db += pn - mn;
-                    if (row > tok) dG -= beta * (pn - mn);
+                if (t >= w) {  // i = row, j = tok
+                    const float d = row >= tok ? fast_exp2(-up) : 0.0f;
+                    const float snp = z.scale * d * np_low[t][r];
+                    const float fl = row > tok ? d * n_low[t][r] : 0.0f;
+                    const float x = snp * (qk_low[r] * (gq[r] * kscale)) - fl * kkv;
+                    cl = snp * beta;
+                    f += fl * beta;
+                    db += x;
+                    dG -= row > tok ? x * beta : 0.0f;
                 }
                 // times the row scales that K^T and Q^T lack
                 np_up[t][r] = cu * gk[r];
@@ -1310,7 +1321,7 @@ __global__ __launch_bounds__(256) void k_delta_grads(const Sizes z, const void* 
         }
         const float uu = fitting(over_wave(mu)), ul = fitting(over_wave(ml)),
                     uf = fitting(over_wave(mf));
-        const float du = 1.0f / uu, dl = 1.0f / ul, df = 1.0f / uf;
+        const float du = fast_rcp(uu), dl = fast_rcp(ul), df = fast_rcp(uf);
         Frag<NS> up[CS], low[CS], f[CS];
 #pragma unroll
         for (int cs = 0; cs < CS; ++cs) {
@@ -1320,11 +1331,13 @@ __global__ __launch_bounds__(256) void k_delta_grads(const Sizes z, const void* 
         }
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
+            if (m % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+            const _Float16 *KT = here(ws.KT + kbase), *QT = here(ws.QT + kbase);
             f32x4 a = {}, b = {}, e = {};
 #pragma unroll
             for (int cs = 0; cs < CS; ++cs) {
-                const Frag<NX> kt = load_frag<NX>(ws.KT + kbase, m * CS + cs, lane);
-                const Frag<NX> qt = load_frag<NX>(ws.QT + kbase, m * CS + cs, lane);
+                const Frag<NX> kt = load_frag<NX>(KT, m * CS + cs, lane);
+                const Frag<NX> qt = load_frag<NX>(QT, m * CS + cs, lane);
                 mma(a, kt, up[cs]);
                 mma(b, qt, low[cs]);
                 mma(e, kt, f[cs]);
@@ -1334,23 +1347,16 @@ __global__ __launch_bounds__(256) void k_delta_grads(const Sizes z, const void* 
         }
         dG -= wi;
         // sums over the four lane groups of a token, then over the chunk
-#pragma unroll
-        for (int s = 16; s < 64; s *= 2) {
-            dG += __shfl_xor(dG, s);
-            db += __shfl_xor(db, s);
-        }
-#pragma unroll
-        for (int s = 1; s < 64; s *= 2) {
-            wi += __shfl_xor(wi, s);
-            dot += __shfl_xor(dot, s);
-        }
+        dG = sum_groups(dG);
+        db = sum_groups(db);
+        wi = sum_wave(wi);
+        dot = sum_wave(dot);
         if (g == 0) sdg[tok] = dG;
         if (lane == 0) {
             swave[w][0] = wi;
             swave[w][1] = dot;
         }
-        const int64_t at = (c.token + tok) * z.heads_v + h;
-        if (g == 0 && has) dbp[at] = db;
+        if (g == 0 && tok < c.n) dbp[(c.token + tok) * z.heads_v + h] = db;
         __syncthreads();
         if (w == 0) {
             float end = 0.0f, sd = 0.0f;
@@ -1377,19 +1383,13 @@ __global__ __launch_bounds__(256) void k_delta_grads(const Sizes z, const void* 
         }
         __syncthreads();
     }
-    if (has) {
-        const int64_t to = ((c.token + tok) * z.heads_k + hk) * z.dk;
-        In* dqr = static_cast<In*>(dqp) + to;
-        In* dkr = static_cast<In*>(dkp) + to;
+    if (tok < c.n) {
+        const int64_t to = ((c.token + tok) * z.heads_k + hk) * z.dk + 4 * g;
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
-            const int k0 = 16 * m + 4 * g;
-            if (k0 < z.dk) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    dqr[k0 + i] = from_f32<In>(dq[m][i]);
-                    dkr[k0 + i] = from_f32<In>(dk[m][i]);
-                }
+            if (16 * m + 4 * g < z.dk) {
+                store4(static_cast<In*>(dqp) + to + 16 * m, dq[m]);
+                store4(static_cast<In*>(dkp) + to + 16 * m, dk[m]);
             }
         }
     }
