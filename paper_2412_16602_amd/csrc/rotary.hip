@@ -4,14 +4,19 @@
 // Pair j of a head turns by theta = position[axis(j)] * inv_freq[j]. A
 // workgroup takes a run of tokens: it forms the cosines and sines of its
 // (token, pair) angles once, in LDS, and its threads then pass over the
-// tokens' heads (both tensors), lanes_per_head lanes to a head, each holding
-// the two vectors of V elements that V pairs need. The angle is formed and
-// reduced to one turn in binary64 (exact products: 31-bit positions of
-// 24-bit frequencies), because in binary32 a position of 10^4 would already
-// cost 10^-3 of a radian.
+// tokens' heads (both tensors), an item of V pairs (two vectors) or V plain
+// elements at a time. The angle is formed and reduced to one turn in binary64
+// (exact products: 31-bit positions of 24-bit frequencies), because in
+// binary32 a position of 10^4 would already cost 10^-3 of a radian.
 //
-// Bound by HBM: each element is read and written once (twice read backward
-// with the norm); the sums of the norm are shuffles within a head's lanes.
+// Bound by memory: each element is read and written once (backward with the
+// norm, two read). Without the norm the items of a run lie in a row over the
+// threads, whatever their number in a head is, and four are in flight in each;
+// 2 x 16x28x28 tokens, 12 + 4 heads of 128 with 60 pairs, bf16 (206 MB in and
+// out): 39 us, 5.2 TB/s, as fast as a copy; a power of two of lanes to a head
+// (17 items in 32 lanes) took 58. With the norm its sums are shuffles within a
+// head's lanes; 32 x 56x56 tokens, 3 + 3 heads of 64, fp32, backward (462 MB):
+// 92 us, 5.0 TB/s.
 #include "vmb_internal.h"
 
 namespace vmb {
@@ -54,19 +59,16 @@ __device__ __forceinline__ void store(T* p, const float (&f)[V]) {
     *reinterpret_cast<Vec<T, V>*>(p) = x;
 }
 
-template <typename T, int V, bool kNorm, bool kBack>
-__global__ __launch_bounds__(kThreads) void k_rotary(const RotaryDev a) {
-    __shared__ float2 table[kTableMax];
-  for (int64_t run = blockIdx.x; run < a.runs; run += gridDim.x) {
-    const int64_t t0 = run * a.tile;
-    const int n_tok = static_cast<int>(a.tokens - t0 < a.tile ? a.tokens - t0 : a.tile);
+// Cosines and sines of a run of tokens (backward: the turn back).
+template <bool kBack>
+__device__ __forceinline__ void fill_table(const RotaryDev& a, float2* table, int64_t t0,
+                                           int n_tok) {
     for (int e = threadIdx.x; e < n_tok * a.pairs; e += kThreads) {
         const int tok = e / a.pairs, j = e - tok * a.pairs;
         const int64_t t = t0 + tok, b = t / a.L;
         int axis = 0;
         while (axis < a.n_axes - 1 && j >= a.section_end[axis]) ++axis;
-        const int32_t pos =
-            a.positions[b * a.pos_batch_stride + (t - b * a.L) * a.n_axes + axis];
+        const int32_t pos = a.positions[b * a.pos_batch_stride + (t - b * a.L) * a.n_axes + axis];
         constexpr double kTurn = 6.283185307179586476925;
         const double angle = static_cast<double>(pos) * static_cast<double>(a.inv_freq[j]);
         const double turns = rint(angle * (1.0 / kTurn));
@@ -74,74 +76,153 @@ __global__ __launch_bounds__(kThreads) void k_rotary(const RotaryDev a) {
         sincosf(static_cast<float>(__builtin_fma(-turns, kTurn, angle)), &s, &c);
         table[e] = make_float2(c, kBack ? -s : s);
     }
-    __syncthreads();
+}
 
-    const int lanes = 1 << a.lanes_log2;
-    const int lane = threadIdx.x & (lanes - 1);
+// Offsets of an item's two vectors in its head: true for V pairs, false for V
+// elements past the last pair (one vector).
+template <int V>
+__device__ __forceinline__ bool place(const RotaryDev& a, int item, int& o1, int& o2) {
     const int pair_items = a.pairs / V;
-    const int tasks = n_tok * a.heads;
-    for (int task = threadIdx.x >> a.lanes_log2; task < tasks;
-         task += kThreads >> a.lanes_log2) {
-        const int tok = task / a.heads, h = task - tok * a.heads;
+    if (item < pair_items) {
+        o1 = a.interleaved ? 2 * V * item : V * item;
+        o2 = a.interleaved ? o1 + V : a.pairs + V * item;
+        return true;
+    }
+    o1 = 2 * a.pairs + V * (item - pair_items);
+    o2 = o1;
+    return false;
+}
+
+// Turns an item's pairs in place; cs: the angles of its V pairs.
+template <int V>
+__device__ __forceinline__ void turn(const RotaryDev& a, const float2* cs, float (&u)[V],
+                                     float (&w)[V]) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const float2 c = cs[i];
+        if (a.interleaved && V > 1) {
+            // pairs lie side by side: (u0, u1), (u2, u3), .. then w
+            constexpr int kHalf = V > 1 ? V / 2 : 1;
+            float(&s)[V] = i < kHalf ? u : w;
+            const int k = 2 * (i % kHalf);
+            const float p = s[k], q = s[(k + 1) % V];
+            s[k] = p * c.x - q * c.y;
+            s[(k + 1) % V] = p * c.y + q * c.x;
+        } else {
+            const float p = u[i], q = w[i];
+            u[i] = p * c.x - q * c.y;
+            w[i] = p * c.y + q * c.x;
+        }
+    }
+}
+
+// e / d for 0 <= e < 2^24, inv = 1.0f / d: the product is less than one off.
+__device__ __forceinline__ int quotient(int e, int d, float inv) {
+    const int q = static_cast<int>(static_cast<float>(e) * inv), r = e - q * d;
+    return q + (r >= d) - (r < 0);
+}
+
+// Where a token's head h (of both tensors) is read, and written.
+template <typename T, bool kBack>
+struct Head {
+    const T *x, *in;
+    T* y;
+    __device__ __forceinline__ Head(const RotaryDev& a, int64_t t, int h) {
         const bool first = h < a.heads_q;
         const int hh = first ? h : h - a.heads_q;
-        const int64_t t = t0 + tok;
-        const int64_t flat = t * ((first ? a.heads_q : a.heads - a.heads_q)) + hh;
-        const int64_t at_strided =
+        const int64_t at = (t * (first ? a.heads_q : a.heads - a.heads_q) + hh) * a.dim;
+        const int64_t strided =
             t * (first ? a.q_stride : a.k_stride) + static_cast<int64_t>(hh) * a.dim;
-        const int64_t at = flat * a.dim;
-        const T* x = static_cast<const T*>(first ? a.xq : a.xk) + (kBack ? at : at_strided);
-        const T* in = static_cast<const T*>(first ? a.inq : a.ink) + at_strided;
-        T* y = static_cast<T*>(first ? a.yq : a.yk) + at;
-        const float2* cs = table + tok * a.pairs;
+        x = static_cast<const T*>(first ? a.xq : a.xk) + (kBack ? at : strided);
+        in = static_cast<const T*>(first ? a.inq : a.ink) + strided;
+        y = static_cast<T*>(first ? a.yq : a.yk) + at;
+    }
+};
 
-        // offsets of an item's two vectors (the second is absent past the pairs)
-        auto place = [&](int item, int& o1, int& o2) {
-            if (item < pair_items) {
-                o1 = a.interleaved ? 2 * V * item : V * item;
-                o2 = a.interleaved ? o1 + V : a.pairs + V * item;
-                return true;
-            }
-            o1 = 2 * a.pairs + V * (item - pair_items);
-            o2 = o1;
-            return false;
-        };
-        // turns the item's pairs in place
-        auto turn = [&](int item, float (&u)[V], float (&w)[V]) {
+// Without the norm: the (token, head, item) triples of a run in a row over the
+// threads, kAhead of them in flight in each.
+template <typename T, int V, bool kBack>
+__global__ __launch_bounds__(kThreads) void k_rotary_flat(const RotaryDev a) {
+    constexpr int kAhead = 4;
+    __shared__ float2 table[kTableMax];
+    const float items_inv = 1.0f / static_cast<float>(a.items);
+    const float heads_inv = 1.0f / static_cast<float>(a.heads);
+    for (int64_t run = blockIdx.x; run < a.runs; run += gridDim.x) {
+        const int64_t t0 = run * a.tile;
+        const int n_tok = static_cast<int>(a.tokens - t0 < a.tile ? a.tokens - t0 : a.tile);
+        const int count = n_tok * a.heads * a.items;
+        // the first values are on their way while the angles are formed
+        float u[kAhead][V], w[kAhead][V];
+        T* y1[kAhead];
+        T* y2[kAhead];
+        const float2* cs[kAhead];
+        auto fetch = [&](int base) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float2 c = cs[V * item + i];
-                if (a.interleaved && V > 1) {
-                    // pairs lie side by side: (u0, u1), (u2, u3), .. then w
-                    constexpr int kHalf = V > 1 ? V / 2 : 1;
-                    float(&s)[V] = i < kHalf ? u : w;
-                    const int k = 2 * (i % kHalf);
-                    const float p = s[k], q = s[(k + 1) % V];
-                    s[k] = p * c.x - q * c.y;
-                    s[(k + 1) % V] = p * c.y + q * c.x;
-                } else {
-                    const float p = u[i], q = w[i];
-                    u[i] = p * c.x - q * c.y;
-                    w[i] = p * c.y + q * c.x;
-                }
+            for (int k = 0; k < kAhead; ++k) {
+                int e = base + static_cast<int>(threadIdx.x) + k * kThreads;
+                e = e < count ? e : count - 1;
+                const int task = quotient(e, a.items, items_inv);
+                const int tok = quotient(task, a.heads, heads_inv);
+                const int item = e - task * a.items;
+                const Head<T, kBack> h(a, t0 + tok, task - tok * a.heads);
+                int o1, o2;
+                const bool pair = place<V>(a, item, o1, o2);
+                load<T, V>(h.x + o1, u[k]);
+                load<T, V>(h.x + o2, w[k]);
+                y1[k] = h.y + o1;
+                y2[k] = h.y + o2;
+                cs[k] = pair ? table + tok * a.pairs + V * item : nullptr;
             }
         };
-
-        float u[V], w[V], xu[V], xw[V];
-        float sq = 0.0f, dot = 0.0f;
-        // the item's values, turned (backward: turned gradients, and the
-        // inputs in xu, xw); adds to the sums
-        auto fetch = [&](int item) {
-            int o1, o2;
-            const bool pair = place(item, o1, o2);
-            load<T, V>(x + o1, u);
-            if (pair) load<T, V>(x + o2, w);
-            if constexpr (kNorm && kBack) {
-                load<T, V>(in + o1, xu);
-                if (pair) load<T, V>(in + o2, xw);
+        fetch(0);
+        fill_table<kBack>(a, table, t0, n_tok);
+        __syncthreads();
+        for (int base = 0; base < count; base += kAhead * kThreads) {
+            if (base) fetch(base);
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                if (base + static_cast<int>(threadIdx.x) + k * kThreads >= count) continue;
+                if (cs[k]) {
+                    turn<V>(a, cs[k], u[k], w[k]);
+                    store<T, V>(y2[k], w[k]);
+                }
+                store<T, V>(y1[k], u[k]);
             }
-            if (pair) turn(item, u, w);
-            if constexpr (kNorm) {
+        }
+        __syncthreads();  // the table is written again
+    }
+}
+
+// With the norm: lanes_per_head lanes to a head, whose sums are shuffles.
+template <typename T, int V, bool kBack>
+__global__ __launch_bounds__(kThreads) void k_rotary_norm(const RotaryDev a) {
+    __shared__ float2 table[kTableMax];
+    for (int64_t run = blockIdx.x; run < a.runs; run += gridDim.x) {
+        const int64_t t0 = run * a.tile;
+        const int n_tok = static_cast<int>(a.tokens - t0 < a.tile ? a.tokens - t0 : a.tile);
+        fill_table<kBack>(a, table, t0, n_tok);
+        __syncthreads();
+        const int lanes = 1 << a.lanes_log2;
+        const int lane = threadIdx.x & (lanes - 1);
+        const int tasks = n_tok * a.heads;
+        for (int task = threadIdx.x >> a.lanes_log2; task < tasks;
+             task += kThreads >> a.lanes_log2) {
+            const int tok = task / a.heads;
+            const Head<T, kBack> h(a, t0 + tok, task - tok * a.heads);
+            float u[V], w[V], xu[V], xw[V];
+            float sq = 0.0f, dot = 0.0f;
+            // the item's values, turned (backward: turned gradients, and the
+            // inputs in xu, xw); adds to the sums
+            auto fetch = [&](int item) {
+                int o1, o2;
+                const bool pair = place<V>(a, item, o1, o2);
+                load<T, V>(h.x + o1, u);
+                if (pair) load<T, V>(h.x + o2, w);
+                if constexpr (kBack) {
+                    load<T, V>(h.in + o1, xu);
+                    if (pair) load<T, V>(h.in + o2, xw);
+                }
+                if (pair) turn<V>(a, table + tok * a.pairs + V * item, u, w);
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
                     // a rotation keeps the length, so the forward sums the
@@ -155,60 +236,51 @@ __global__ __launch_bounds__(kThreads) void k_rotary(const RotaryDev a) {
                         if (kBack) dot = __builtin_fmaf(q, w[i], dot);
                     }
                 }
-            }
-        };
-        auto put = [&](int item, float r, float m) {
-            int o1, o2;
-            const bool pair = place(item, o1, o2);
-            if constexpr (kNorm) {
+            };
+            auto put = [&](int item, float r, float m) {
+                int o1, o2;
+                const bool pair = place<V>(a, item, o1, o2);
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
                     u[i] = kBack ? r * (u[i] - xu[i] * m) : r * u[i];
                     if (pair) w[i] = kBack ? r * (w[i] - xw[i] * m) : r * w[i];
                 }
-            }
-            store<T, V>(y + o1, u);
-            if (pair) store<T, V>(y + o2, w);
-        };
+                store<T, V>(h.y + o1, u);
+                if (pair) store<T, V>(h.y + o2, w);
+            };
 
-        if (lane < a.items) fetch(lane);
-        float r = 1.0f, m = 0.0f;
-        if constexpr (kNorm) {
+            if (lane < a.items) fetch(lane);
             for (int item = lane + lanes; item < a.items; item += lanes) fetch(item);
             for (int k = lanes / 2; k > 0; k /= 2) {
                 sq += __shfl_xor(sq, k);
                 if (kBack) dot += __shfl_xor(dot, k);
             }
-            r = 1.0f / sqrtf(sq + a.eps);
-            m = dot * r * r;
-        }
-        // heads of more items than lanes: the others are fetched again
-        if (a.items > lanes) {
-            for (int item = lane; item < a.items; item += lanes) {
-                fetch(item);
-                put(item, r, m);
+            const float r = 1.0f / sqrtf(sq + a.eps), m = dot * r * r;
+            // heads of more items than lanes: the others are fetched again
+            if (a.items > lanes) {
+                for (int item = lane; item < a.items; item += lanes) {
+                    fetch(item);
+                    put(item, r, m);
+                }
+            } else if (lane < a.items) {
+                put(lane, r, m);
             }
-        } else if (lane < a.items) {
-            put(lane, r, m);
         }
+        __syncthreads();  // the table is written again
     }
-    __syncthreads();  // the table is written again
-  }
 }
 
 template <typename T, int V>
 void launch_v(const RotaryDev& d, bool norm, bool back, hipStream_t s) {
     constexpr int64_t kMostGroups = 1 << 22;  // a grid holds 2^32 threads; further runs follow
     const dim3 grid(static_cast<unsigned>(d.runs < kMostGroups ? d.runs : kMostGroups));
-    if (back) {
-        if (norm)
-            k_rotary<T, V, true, true><<<grid, kThreads, 0, s>>>(d);
-        else
-            k_rotary<T, V, false, true><<<grid, kThreads, 0, s>>>(d);
-    } else if (norm) {
-        k_rotary<T, V, true, false><<<grid, kThreads, 0, s>>>(d);
+    if (norm) {
+        if (back) k_rotary_norm<T, V, true><<<grid, kThreads, 0, s>>>(d);
+        else k_rotary_norm<T, V, false><<<grid, kThreads, 0, s>>>(d);
+    } else if (back) {
+        k_rotary_flat<T, V, true><<<grid, kThreads, 0, s>>>(d);
     } else {
-        k_rotary<T, V, false, false><<<grid, kThreads, 0, s>>>(d);
+        k_rotary_flat<T, V, false><<<grid, kThreads, 0, s>>>(d);
     }
 }
 
@@ -253,7 +325,10 @@ vmb_status launch_rotary(const RotaryArgs& a, bool backward) {
     // enough work to pay for the angles
     int64_t tile = (d.tokens + 2047) / 2048;
     const int64_t most = kTableMax / d.pairs < 16 ? kTableMax / d.pairs : 16;
-    d.tile = static_cast<int>(tile > most ? most : tile);
+    tile = tile > most ? most : tile;
+    // the triples of a run stay below 2^24 (those of a token are below 2^23)
+    while (tile * d.heads * d.items >= 1 << 24) tile /= 2;
+    d.tile = static_cast<int>(tile);
     d.runs = (d.tokens + d.tile - 1) / d.tile;
     if (a.dt == VMB_BF16) {
         if (v == 8) launch_v<bf16_t, 8>(d, norm, backward, a.stream);
