@@ -3,19 +3,31 @@
 //
 // x [batch, P, C], a group is c = C / groups neighbouring channels of all P
 // pixels of an image. Threads own vectors of V channels (16 bytes where C
-// allows) and pass down the pixels of their run, so every load of a wave is a
-// piece of whole rows whatever c is; what they gather is kept per channel and
-// joined into groups by a second, small kernel over [image, run, channel]
-// partial results; a third pass writes the output. Each pass is bound by
-// memory; the last one finds its inputs in the 256 MB last-level cache where
-// they fit.
+// allows) and pass down the pixels, so every load is a piece of rows whatever
+// c is; what they gather is kept per channel and joined into groups.
 //
-// Forward statistics: a thread takes kRun pixels at a time, forms their mean
-// and centred sum of squares from the registers and joins them to its running
-// ones (mean += d n_b / n, M2 += M2_b + d^2 n_a n_b / n). All values are taken
-// less a value of their group (its first channel in the first pixel), an
-// exact subtraction where an offset is large against the spread, so an offset
-// costs no accuracy. Backward sums: sum dz and sum dz xhat per channel.
+// Two forms:
+// - Forward, in registers (k_gn_held): a workgroup takes whole groups of an
+//   image, CB channels, and holds all of their values, up to ten vectors a
+//   thread: x is read once, the mean, the centred sum of squares and the output
+//   come from the registers. The blocks of an image go to one XCD, whose L2
+//   joins the pieces of its rows. 32 x 56x56, 192 channels, 32 groups, bf16
+//   (77 MB in and out): 28 us, the passes 34. A workgroup fills a compute unit,
+//   so its loads, its arithmetic and its stores follow each other; the
+//   arithmetic (about 20 instructions a value) is the longest of the three.
+// - In three passes otherwise: statistics of runs of pixels per channel, a
+//   small kernel that joins them over [image, run, channel], then the output.
+//   Bound by memory: 2 x 128x512, 192 channels, fp32, backward (x and dy read
+//   twice, 503 MB in all): 33 + 6 + 49 us, the outer two at 6 TB/s. Held
+//   backward, x and dy take twice the registers; that spilled and lost (32 x
+//   56x56, bf16: 75 us, the passes 55).
+//
+// Forward statistics of the passes: a thread takes kRun pixels at a time, forms
+// their mean and centred sum of squares from the registers and joins them to
+// its running ones (mean += d n_b / n, M2 += M2_b + d^2 n_a n_b / n). All values
+// are taken less a value of their group (its first channel in the first
+// pixel), an exact subtraction where an offset is large against the spread, so
+// an offset costs no accuracy. Backward sums: sum dz and sum dz xhat per channel.
 #include "vmb_internal.h"
 
 namespace vmb {
@@ -52,16 +64,21 @@ __device__ __forceinline__ float origin(const GnDev& a, int64_t base, int ch) {
     return to_f32(static_cast<const T*>(a.x)[base + ch / a.c * a.c]);
 }
 
+// sigmoid(z): the reciprocal instruction is within one unit of the last place,
+// where a division takes ten instructions.
+__device__ __forceinline__ float sigmoid(float z) {
+    return __builtin_amdgcn_rcpf(1.0f + __expf(-z));
+}
 template <bool kSilu>
 __device__ __forceinline__ float activate(float z) {
-    return kSilu ? z / (1.0f + __expf(-z)) : z;
+    return kSilu ? z * sigmoid(z) : z;
 }
 // act'(z)
 template <bool kSilu>
 __device__ __forceinline__ float slope(float z) {
     if (!kSilu) return 1.0f;
-    const float s = 1.0f / (1.0f + __expf(-z));
-    return s * (1.0f + z * (1.0f - s));
+    const float s = sigmoid(z);
+    return s * __builtin_fmaf(z, 1.0f - s, 1.0f);
 }
 
 // Joins the rows of threads of a workgroup channel by channel (fixed order)
@@ -69,8 +86,7 @@ __device__ __forceinline__ float slope(float z) {
 // Forward: (mean, M2) of n values; backward: two plain sums.
 template <int V, bool kMoments>
 __device__ __forceinline__ void join_rows(const GnDev& a, float n, const float (&p)[V],
-                                          const float (&q)[V], int vec, int row, bool on,
-                                          float* out) {
+                                          const float (&q)[V], int v0, float* out) {
     __shared__ float sp[kThreads * V], sq[kThreads * V], sn[kThreads];
     const int tid = threadIdx.x;
 #pragma unroll
@@ -80,30 +96,29 @@ __device__ __forceinline__ void join_rows(const GnDev& a, float n, const float (
     }
     sn[tid] = n;
     __syncthreads();
-    if (on && row == 0) {
-        const int step = a.vectors < kThreads ? a.vectors : kThreads;
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            float m = sp[i * kThreads + tid], s = sq[i * kThreads + tid], k = n;
-            for (int r = 1; r < a.rows; ++r) {
-                const int at = tid + r * step;
-                const float mb = sp[i * kThreads + at], qb = sq[i * kThreads + at];
-                if constexpr (kMoments) {
-                    const float nb = sn[at], d = mb - m, t = k + nb;
-                    if (nb > 0.0f) {
-                        const float f = nb / t;
-                        m += d * f;
-                        s += qb + d * d * k * f;
-                        k = t;
-                    }
-                } else {
-                    m += mb;
-                    s += qb;
+    // a thread to a channel: channel e is element e % V of the vector v0 + e / V
+    const int step = a.vectors < kThreads ? a.vectors : kThreads;
+    const int left = a.vectors - v0 < step ? a.vectors - v0 : step;
+    for (int e = tid; e < left * V; e += kThreads) {
+        const int at0 = e % V * kThreads + e / V;
+        float m = sp[at0], s = sq[at0], k = sn[e / V];
+        for (int r = 1; r < a.rows; ++r) {
+            const float mb = sp[at0 + r * step], qb = sq[at0 + r * step];
+            if constexpr (kMoments) {
+                const float nb = sn[e / V + r * step], d = mb - m, t = k + nb;
+                if (nb > 0.0f) {
+                    const float f = nb * __builtin_amdgcn_rcpf(t);
+                    m = __builtin_fmaf(d, f, m);
+                    s += qb + d * d * k * f;
+                    k = t;
                 }
+            } else {
+                m += mb;
+                s += qb;
             }
-            out[2 * (vec * V + i)] = m;
-            out[2 * (vec * V + i) + 1] = s;
         }
+        out[2 * (v0 * V + e)] = m;
+        out[2 * (v0 * V + e) + 1] = s;
     }
     __syncthreads();
 }
@@ -165,7 +180,7 @@ __global__ __launch_bounds__(kThreads) void k_gn_part(const GnDev a) {
                 const int ch = on ? vec * V + i : 0, g = ch / a.c;
                 mu[i] = a.mean[img * a.groups + g];
                 rs[i] = a.rstd[img * a.groups + g];
-                ga[i] = a.gamma ? a.gamma[ch] : 1.0f;
+                ga[i] = (a.gamma ? a.gamma[ch] : 1.0f) * rs[i];
                 be[i] = a.beta ? a.beta[ch] : 0.0f;
             }
             for (int64_t at = p0 + row; on && at < p1; at += kRun * a.rows) {
@@ -181,31 +196,32 @@ __global__ __launch_bounds__(kThreads) void k_gn_part(const GnDev a) {
                     const bool in = at + k * a.rows < p1;
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
-                        const float xh = (to_f32(bx[k].v[i]) - mu[i]) * rs[i];
+                        const float off = to_f32(bx[k].v[i]) - mu[i];
                         float d = to_f32(bd[k].v[i]);
-                        if (kSilu) d *= slope<kSilu>(__builtin_fmaf(xh, ga[i], be[i]));
+                        if (kSilu) d *= slope<kSilu>(__builtin_fmaf(off, ga[i], be[i]));
                         if (in) {
                             p[i] += d;
-                            q[i] = __builtin_fmaf(d, xh, q[i]);
+                            q[i] = __builtin_fmaf(d, off, q[i]);
                         }
                     }
                 }
             }
+#pragma unroll
+            for (int i = 0; i < V; ++i) q[i] *= rs[i];
         }
-        join_rows<V, !kBack>(a, n, p, q, vec, row, on, part);
+        join_rows<V, !kBack>(a, n, p, q, v0, part);
     }
 }
 
-// Sum of v over a workgroup, in a fixed order.
+// Sum of v over a workgroup of up to 1024 threads, in a fixed order.
 __device__ __forceinline__ float total(float v) {
-    __shared__ float red[kThreads / 64];
+    __shared__ float red[16];
     for (int k = 32; k > 0; k /= 2) v += __shfl_xor(v, k);
     __syncthreads();
     if (threadIdx.x % 64 == 0) red[threadIdx.x / 64] = v;
     __syncthreads();
     float t = 0.0f;
-#pragma unroll
-    for (int w = 0; w < kThreads / 64; ++w) t += red[w];
+    for (unsigned w = 0; w < blockDim.x / 64; ++w) t += red[w];
     return t;
 }
 
@@ -218,20 +234,22 @@ __device__ __forceinline__ float held(const GnDev& a, int s) {
 // Statistics of one (group, image) from its channels' partial ones: the mean
 // of the means, then the sums of squares about it.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void k_gn_join(const GnDev a, float* stat, float* mean,
+__global__ __launch_bounds__(1024) void k_gn_join(const GnDev a, float* stat, float* mean,
                                                       float* rstd) {
     const int g = blockIdx.x, img = blockIdx.y;
     const float* part = a.part + static_cast<int64_t>(img) * a.splits * a.C * 2;
     const int n = a.c * a.splits;
     const float count = static_cast<float>(a.P) * static_cast<float>(a.c);
     float s = 0.0f;
-    for (int e = threadIdx.x; e < n; e += kThreads) {
+#pragma unroll 8
+    for (int e = threadIdx.x; e < n; e += static_cast<int>(blockDim.x)) {
         const int sp = e / a.c, ch = g * a.c + e - sp * a.c;
         s += held(a, sp) * part[2 * (static_cast<int64_t>(sp) * a.C + ch)];
     }
     const float mu = total(s) / count;
     s = 0.0f;
-    for (int e = threadIdx.x; e < n; e += kThreads) {
+#pragma unroll 8
+    for (int e = threadIdx.x; e < n; e += static_cast<int>(blockDim.x)) {
         const int sp = e / a.c, ch = g * a.c + e - sp * a.c;
         const float* q = part + 2 * (static_cast<int64_t>(sp) * a.C + ch);
         const float d = q[0] - mu;
@@ -249,10 +267,38 @@ __global__ __launch_bounds__(kThreads) void k_gn_join(const GnDev a, float* stat
     }
 }
 
+// Gradients of gamma and beta of kJoinChannels channels: the sums over count
+// partial results.
+constexpr int kJoinChannels = 8;
+__device__ __forceinline__ void join_affine(const float* part, int64_t count, int C, int c0,
+                                            float* dgamma, float* dbeta) {
+    __shared__ float r1[1024], r2[1024];
+    const int ch = c0 + threadIdx.x % kJoinChannels, rows = blockDim.x / kJoinChannels;
+    float s1 = 0.0f, s2 = 0.0f;
+    if (ch < C) {
+#pragma unroll 4
+        for (int64_t e = threadIdx.x / kJoinChannels; e < count; e += rows) {
+            s1 += part[2 * (e * C + ch)];
+            s2 += part[2 * (e * C + ch) + 1];
+        }
+    }
+    r1[threadIdx.x] = s1;
+    r2[threadIdx.x] = s2;
+    __syncthreads();
+    if (threadIdx.x < kJoinChannels && ch < C) {
+#pragma unroll 8
+        for (int r = 1; r < rows; ++r) {
+            s1 += r1[threadIdx.x + r * kJoinChannels];
+            s2 += r2[threadIdx.x + r * kJoinChannels];
+        }
+        dbeta[ch] = s1;
+        dgamma[ch] = s2;
+    }
+}
+
 // Backward: blocks below batch * groups form a group's two means; the rest
-// the gradients of gamma and beta of 32 channels over all images.
-constexpr int kJoinChannels = 32;
-__global__ __launch_bounds__(kThreads) void k_gn_join_bwd(const GnDev a, int batch, float* stat,
+// the gradients of gamma and beta over all images.
+__global__ __launch_bounds__(1024) void k_gn_join_bwd(const GnDev a, int batch, float* stat,
                                                           float* dgamma, float* dbeta) {
     const int sums = batch * a.groups;
     const int b = blockIdx.x;
@@ -260,7 +306,8 @@ __global__ __launch_bounds__(kThreads) void k_gn_join_bwd(const GnDev a, int bat
         const int img = b / a.groups, g = b - img * a.groups;
         const float* part = a.part + static_cast<int64_t>(img) * a.splits * a.C * 2;
         float s1 = 0.0f, s2 = 0.0f;
-        for (int e = threadIdx.x; e < a.c * a.splits; e += kThreads) {
+#pragma unroll 8
+        for (int e = threadIdx.x; e < a.c * a.splits; e += static_cast<int>(blockDim.x)) {
             const int sp = e / a.c, ch = g * a.c + e - sp * a.c;
             const float* q = part + 2 * (static_cast<int64_t>(sp) * a.C + ch);
             const float ga = a.gamma ? a.gamma[ch] : 1.0f;
@@ -275,26 +322,8 @@ __global__ __launch_bounds__(kThreads) void k_gn_join_bwd(const GnDev a, int bat
         }
         return;
     }
-    __shared__ float r1[kThreads], r2[kThreads];
-    const int ch = (b - sums) * kJoinChannels + threadIdx.x % kJoinChannels;
-    float s1 = 0.0f, s2 = 0.0f;
-    if (ch < a.C)
-        for (int64_t e = threadIdx.x / kJoinChannels; e < static_cast<int64_t>(batch) * a.splits;
-             e += kThreads / kJoinChannels) {
-            s1 += a.part[2 * (e * a.C + ch)];
-            s2 += a.part[2 * (e * a.C + ch) + 1];
-        }
-    r1[threadIdx.x] = s1;
-    r2[threadIdx.x] = s2;
-    __syncthreads();
-    if (threadIdx.x < kJoinChannels && ch < a.C) {
-        for (int r = 1; r < kThreads / kJoinChannels; ++r) {
-            s1 += r1[threadIdx.x + r * kJoinChannels];
-            s2 += r2[threadIdx.x + r * kJoinChannels];
-        }
-        dbeta[ch] = s1;
-        dgamma[ch] = s2;
-    }
+    join_affine(a.part, static_cast<int64_t>(batch) * a.splits, a.C, (b - sums) * kJoinChannels,
+                dgamma, dbeta);
 }
 
 // The output: y = act(xhat gamma + beta), or dx = rstd (dz gamma - m1 - xhat m2).
@@ -313,21 +342,23 @@ __global__ __launch_bounds__(kThreads) void k_gn_apply(const GnDev a, const floa
         const T* x = static_cast<const T*>(a.x) + off;
         const T* dy = static_cast<const T*>(a.dy) + off;
         T* out = static_cast<T*>(a.out) + off;
-        float from[V] = {}, mu[V], rs[V], ga[V], be[V], m1[V], m2[V];
+        // z = (x - from) ga + be; dx = dz ga + (x - from) m2 + m1
+        float from[V], ga[V], be[V], m1[V], m2[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const int ch = vec * V + i, at = img * a.groups + ch / a.c;
-            ga[i] = a.gamma ? a.gamma[ch] : 1.0f;
-            be[i] = a.beta ? a.beta[ch] : 0.0f;
+            const float gamma = a.gamma ? a.gamma[ch] : 1.0f, beta = a.beta ? a.beta[ch] : 0.0f;
             if constexpr (kBack) {
-                mu[i] = a.mean[at];
-                rs[i] = a.rstd[at];
-                m1[i] = stat[2 * at];
-                m2[i] = stat[2 * at + 1];
+                const float rs = a.rstd[at];
+                from[i] = a.mean[at];
+                ga[i] = gamma * rs;
+                be[i] = beta;
+                m1[i] = -rs * stat[2 * at];
+                m2[i] = -rs * rs * stat[2 * at + 1];
             } else {
                 from[i] = origin<T>(a, base, ch);
-                mu[i] = stat[2 * at];
-                rs[i] = stat[2 * at + 1];
+                ga[i] = gamma * stat[2 * at + 1];
+                be[i] = __builtin_fmaf(-stat[2 * at], ga[i], beta);
             }
         }
         for (int64_t at = p0 + row; at < p1; at += kRun * a.rows) {
@@ -341,35 +372,220 @@ __global__ __launch_bounds__(kThreads) void k_gn_apply(const GnDev a, const floa
 #pragma unroll
             for (int k = 0; k < kRun; ++k) {
                 const int64_t pix = at + k * a.rows;
-                if (pix >= p1) break;
                 Vec<T, V> o;
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    const float xh = ((to_f32(bx[k].v[i]) - from[i]) - mu[i]) * rs[i];
-                    const float z = __builtin_fmaf(xh, ga[i], be[i]);
+                    const float off = to_f32(bx[k].v[i]) - from[i];
+                    const float z = __builtin_fmaf(off, ga[i], be[i]);
                     if constexpr (kBack) {
                         const float d = to_f32(bd[k].v[i]) * slope<kSilu>(z);
-                        o.v[i] = from_f32<T>(rs[i] * (d * ga[i] - m1[i] - xh * m2[i]));
+                        o.v[i] = from_f32<T>(
+                            __builtin_fmaf(d, ga[i], __builtin_fmaf(off, m2[i], m1[i])));
                     } else {
                         o.v[i] = from_f32<T>(activate<kSilu>(z));
                     }
                 }
-                *reinterpret_cast<Vec<T, V>*>(out + pix * a.C) = o;
+                if (pix < p1) *reinterpret_cast<Vec<T, V>*>(out + pix * a.C) = o;
             }
         }
     }
 }
 
+// ------------------------------------------------------- held in registers
+
+struct HeldDev {
+    const void* x;
+    const float *gamma, *beta;
+    void* out;
+    float *mean, *rstd;
+    int64_t P;
+    int C, groups, c, blocks, CB, vectors, rows, full, total;  // total = batch * blocks
+    float eps;
+};
+
+// Means over the pixels and channels of each group of a block, in a fixed
+// order. s: sums of this thread's V channels; lds: rows x CB, and the groups.
+template <int V>
+__device__ __forceinline__ void group_means(const HeldDev& a, const float (&s)[V], int row,
+                                            int vec, float* lds, float* means) {
+    const int CB = a.CB, threads = blockDim.x;
+    const int most = threads / CB > 0 ? threads / CB : 1, Q = a.rows < most ? a.rows : most;
+    if (row < a.rows) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) lds[row * CB + vec * V + i] = s[i];
+    }
+    __syncthreads();
+    // every Qth row to the first Q
+    for (int e = threadIdx.x; e < Q * CB; e += threads) {
+        float t = 0.0f;
+#pragma unroll 4
+        for (int at = e; at < a.rows * CB; at += Q * CB) t += lds[at];
+        lds[e] = t;
+    }
+    __syncthreads();
+    // a wave to a group
+    const float inv = 1.0f / (static_cast<float>(a.P) * static_cast<float>(a.c));
+    for (int g = threadIdx.x / 64; g * a.c < CB; g += threads / 64) {
+        float t = 0.0f;
+        for (int e = threadIdx.x % 64; e < Q * a.c; e += 64) {
+            const int q = e / a.c;
+            t += lds[q * CB + g * a.c + e - q * a.c];
+        }
+        for (int k = 32; k > 0; k /= 2) t += __shfl_xor(t, k);
+        if (threadIdx.x % 64 == 0) means[g] = t * inv;
+    }
+    __syncthreads();
+}
+
+// N vectors a thread. Dynamic LDS: rows x CB, then CB floats.
+template <typename T, int V, int N, bool kSilu>
+__global__ __launch_bounds__(1024) void k_gn_held(const HeldDev a) {
+    extern __shared__ float lds[];
+    float* means = lds + a.rows * a.CB;
+    // blocks of an image on one XCD: the 1-D grid is dealt to the XCDs in turn
+    const int per = (a.total + 7) / 8;
+    const int b = static_cast<int>(blockIdx.x % 8) * per + static_cast<int>(blockIdx.x / 8);
+    if (b >= a.total) return;
+    const int img = b / a.blocks, ch0 = (b - img * a.blocks) * a.CB;
+    const int row = threadIdx.x / a.vectors, vec = threadIdx.x - row * a.vectors;
+    const int64_t base = static_cast<int64_t>(img) * a.P * a.C + ch0 + vec * V;
+    const T* x = static_cast<const T*>(a.x) + base;
+    // full whole rounds of rows, and one that may end early; threads past the
+    // rows read the first pixel's vector and write nothing
+    const bool on = row < a.rows;
+    const bool last = on && row + static_cast<int64_t>(a.full) * a.rows < a.P;
+    Vec<T, V> bx[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const bool in = k < a.full ? on : k == a.full && last;
+        bx[k] = load<T, V>(in ? x + (row + static_cast<int64_t>(k) * a.rows) * a.C : x);
+    }
+    int gr[V];  // groups, in the block, of this thread's channels
+    float from[V], ga[V], be[V], s[V], mu[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const int ch = ch0 + vec * V + i;
+        gr[i] = (vec * V + i) / a.c;
+        ga[i] = a.gamma ? a.gamma[ch] : 1.0f;
+        be[i] = a.beta ? a.beta[ch] : 0.0f;
+        from[i] = to_f32(
+            static_cast<const T*>(a.x)[static_cast<int64_t>(img) * a.P * a.C + ch0 + gr[i] * a.c]);
+        s[i] = 0.0f;
+    }
+    auto each = [&](auto&& f) {
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+            if (k < a.full || (k == a.full && last)) f(k);
+    };
+    each([&](int k) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) s[i] += to_f32(bx[k].v[i]) - from[i];
+    });
+    group_means<V>(a, s, row, vec, lds, means);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        mu[i] = means[gr[i]];
+        s[i] = 0.0f;
+    }
+    each([&](int k) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const float d = (to_f32(bx[k].v[i]) - from[i]) - mu[i];
+            s[i] = __builtin_fmaf(d, d, s[i]);
+        }
+    });
+    __syncthreads();  // the means are written again
+    group_means<V>(a, s, row, vec, lds, means);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const float rs = 1.0f / sqrtf(means[gr[i]] + a.eps);
+        if (a.mean && row == 0 && (vec * V + i) % a.c == 0) {
+            const int at = img * a.groups + ch0 / a.c + gr[i];
+            a.mean[at] = from[i] + mu[i];
+            a.rstd[at] = rs;
+        }
+        ga[i] *= rs;
+        be[i] = __builtin_fmaf(-mu[i], ga[i], be[i]);
+    }
+    if (!on) return;
+    T* out = static_cast<T*>(a.out) + base;
+    each([&](int k) {
+        Vec<T, V> o;
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            o.v[i] = from_f32<T>(
+                activate<kSilu>(__builtin_fmaf(to_f32(bx[k].v[i]) - from[i], ga[i], be[i])));
+        *reinterpret_cast<Vec<T, V>*>(out + (row + static_cast<int64_t>(k) * a.rows) * a.C) = o;
+    });
+}
+
+// How a call is held, if it is: whole groups of CB channels, as many as leave
+// 256 workgroups, that fit the registers and 48 KB of LDS. Few workgroups of
+// many vectors a thread lose to the passes' many (one image of 3136 x 192 in
+// fp32, 8 workgroups of 10: 18 us, the passes 15; 64 workgroups are even).
+struct HeldPlan {
+    int CB = 0, threads = 0, rows = 0, n = 0;
+};
+HeldPlan held_plan(int64_t batch, int64_t P, int64_t C, int64_t groups, int V) {
+    HeldPlan best;
+    const int64_t c = C / groups;
+    for (int64_t k = 1; k <= groups; ++k) {
+        const int64_t CB = k * c;
+        if (groups % k || CB % V || CB / V > 256) continue;
+        if (best.CB && batch * (C / CB) < 256) break;
+        const int64_t vectors = CB / V;
+        // the fewest threads that hold the block in four vectors each, or 1024
+        int64_t threads = 256;
+        while (threads < 1024 && (P + threads / vectors - 1) / (threads / vectors) > 4) threads *= 2;
+        const int64_t most = threads / vectors, rows = most < P ? most : P;
+        const int64_t n = (P + rows - 1) / rows;
+        if (n > 10 || (rows + 1) * CB * 4 > 48 * 1024) continue;
+        if ((batch * (C / CB) + 7) * threads >> 32) continue;  // threads of a grid
+        if (n > 4 && batch * (C / CB) < 64) continue;
+        best = HeldPlan{static_cast<int>(CB), static_cast<int>(threads), static_cast<int>(rows),
+                        static_cast<int>(n)};
+    }
+    return best;
+}
+
+template <typename T, int V, bool kSilu>
+void launch_held_n(const HeldDev& d, const HeldPlan& p, hipStream_t s) {
+    const unsigned grid = static_cast<unsigned>((d.total + 7) / 8 * 8);
+    const unsigned lds = static_cast<unsigned>((d.rows + 1) * d.CB * 4);
+    const dim3 block(static_cast<unsigned>(p.threads));
+    if (p.n <= 2) k_gn_held<T, V, 2, kSilu><<<grid, block, lds, s>>>(d);
+    else if (p.n <= 4) k_gn_held<T, V, 4, kSilu><<<grid, block, lds, s>>>(d);
+    else k_gn_held<T, V, 10, kSilu><<<grid, block, lds, s>>>(d);
+}
+
+template <typename T, int V>
+void launch_held(const GroupNormArgs& g, const HeldPlan& p) {
+    HeldDev d{};
+    d.x = g.x, d.gamma = g.gamma, d.beta = g.beta, d.out = g.out, d.mean = g.mean, d.rstd = g.rstd;
+    d.P = g.P, d.C = static_cast<int>(g.channels), d.groups = static_cast<int>(g.groups);
+    d.c = d.C / d.groups, d.CB = p.CB, d.blocks = d.C / p.CB, d.vectors = p.CB / V;
+    d.rows = p.rows, d.full = static_cast<int>(g.P / p.rows);
+    d.total = static_cast<int>(g.batch) * d.blocks;
+    d.eps = g.eps;
+    if (g.act == VMB_ACT_SILU) launch_held_n<T, V, true>(d, p, g.stream);
+    else launch_held_n<T, V, false>(d, p, g.stream);
+}
+
+// ------------------------------------------------------------- three passes
+
 template <typename T, int V, bool kBack, bool kSilu>
 void launch_act(const GroupNormArgs& g, const GnDev& d, float* stat) {
     const dim3 grid(static_cast<unsigned>(d.splits), static_cast<unsigned>(g.batch));
-    k_gn_part<T, V, kBack, kSilu><<<grid, kThreads, 0, g.stream>>>(d);
+    // the joins take a long list with more threads (one group of 49152 partial
+    // results, with 256 and 1024 threads: 63 and 52 us a call, backward 51 and 34)
+    const unsigned join = d.c * d.splits > 2048 ? 1024 : 256;
+    k_gn_part<T, V, kBack, kBack && kSilu><<<grid, kThreads, 0, g.stream>>>(d);
     if constexpr (kBack) {
         const int64_t ch = g.dgamma ? (d.C + kJoinChannels - 1) / kJoinChannels : 0;
-        k_gn_join_bwd<<<static_cast<unsigned>(g.batch * d.groups + ch), kThreads, 0, g.stream>>>(
+        k_gn_join_bwd<<<static_cast<unsigned>(g.batch * d.groups + ch), join, 0, g.stream>>>(
             d, static_cast<int>(g.batch), stat, g.dgamma, g.dbeta);
     } else {
-        k_gn_join<T><<<dim3(d.groups, static_cast<unsigned>(g.batch)), kThreads, 0, g.stream>>>(
+        k_gn_join<T><<<dim3(d.groups, static_cast<unsigned>(g.batch)), join, 0, g.stream>>>(
             d, stat, g.mean, g.rstd);
     }
     k_gn_apply<T, V, kBack, kSilu><<<grid, kThreads, 0, g.stream>>>(d, stat);
@@ -388,10 +604,10 @@ void launch_v(const GroupNormArgs& g, const GnDev& d, float* stat, bool back) {
     }
 }
 
-// Splits of an image's pixels: about 1024 workgroups in all, runs of at
-// least 32 pixels.
+// Splits of an image's pixels: about 768 workgroups in all, runs of at least
+// 32 pixels.
 int64_t splits_of(int64_t batch, int64_t P) {
-    int64_t s = (1024 + batch - 1) / batch;
+    int64_t s = (768 + batch - 1) / batch;
     const int64_t most = (P + 31) / 32;
     if (s > most) s = most;
     return s < 1 ? 1 : s;
@@ -427,6 +643,21 @@ vmb_status launch_group_norm(const GroupNormArgs& g, bool backward) {
     d.eps = g.eps;
     int v = g.dt == VMB_BF16 ? 8 : 4;
     while (d.C % v) v /= 2;
+    const HeldPlan plan =
+        backward ? HeldPlan{} : held_plan(g.batch, g.P, g.channels, g.groups, v);
+    if (plan.CB) {
+        if (g.dt == VMB_BF16) {
+            if (v == 8) launch_held<bf16_t, 8>(g, plan);
+            else if (v == 4) launch_held<bf16_t, 4>(g, plan);
+            else if (v == 2) launch_held<bf16_t, 2>(g, plan);
+            else launch_held<bf16_t, 1>(g, plan);
+        } else {
+            if (v == 4) launch_held<float, 4>(g, plan);
+            else if (v == 2) launch_held<float, 2>(g, plan);
+            else launch_held<float, 1>(g, plan);
+        }
+        return check_launch();
+    }
     d.vectors = d.C / v;
     d.rows = d.vectors < kThreads ? kThreads / d.vectors : 1;
     const int64_t want = splits_of(g.batch, g.P);
