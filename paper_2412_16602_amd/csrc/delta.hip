@@ -103,12 +103,43 @@ Streams streams_of(void* ws, const Layout& o) {
     return s;
 }
 
-// A walk's grid: a workgroup of one wave to each of cols tiles of columns (four
-// waves of a head together share what they read in L1, but also its 64 bytes a
-// clock, which then bounds them: 32 x 56x56, 64 x 64 states, 195 against 110 us).
-dim3 walk_grid(const Sizes& z, const Segments& sg, int cols) {
-    return dim3(static_cast<unsigned>(z.n_seq * sg.most), static_cast<unsigned>(z.heads_v),
-                static_cast<unsigned>(cols));
+// A workgroup's waves: states of 128 rows in eights of tiles of columns share
+// their operands in LDS where there are more waves than one for each SIMD
+// (32 x 784 tokens, 6 heads of 128 x 128, 1536 waves: 157 us a forward call
+// against 204 with single waves; 8 x 784 tokens, 384 waves: 99 against 76).
+// Narrower states have work for few waves and lose (32 x 784 tokens, 6 heads of
+// 64 x 64, in fours: 96 against 83 us).
+bool in_eights(unsigned x, unsigned y, int cols) {
+    return cols % 8 == 0 && int64_t{x} * y * cols > 1024;
+}
+
+// A walk over cols tiles of columns.
+template <typename In, int DK, WalkKind kKind>
+void walk(const DeltaArgs& a, const Sizes& z, const Segments& sg, const Streams& ws, int cols) {
+    const unsigned x = static_cast<unsigned>(z.n_seq * sg.most), y = static_cast<unsigned>(z.heads_v);
+    if constexpr (DK == 128) {
+        if (in_eights(x, y, cols)) {
+            k_delta_walk<In, DK, kKind, 8><<<dim3(x, y, cols / 8), 512, 0, a.stream>>>(
+                z, sg, a.v, a.h0, a.o, a.hT, ws);
+            return;
+        }
+    }
+    k_delta_walk<In, DK, kKind, 1><<<dim3(x, y, cols), 64, 0, a.stream>>>(z, sg, a.v, a.h0, a.o,
+                                                                       a.hT, ws);
+}
+template <typename In, int DK, bool kIsLocal>
+void walk_back(const DeltaArgs& a, const Sizes& z, const Segments& sg, const Streams& ws) {
+    const unsigned x = static_cast<unsigned>(z.n_seq * sg.most), y = static_cast<unsigned>(z.heads_v);
+    const int cols = z.dvp / 16;
+    if constexpr (DK == 128) {
+        if (in_eights(x, y, cols)) {
+            k_delta_walk_back<In, DK, kIsLocal, 8><<<dim3(x, y, cols / 8), 512, 0, a.stream>>>(
+                z, sg, a.d_o, a.d_hT, a.d_v, a.d_h0, ws);
+            return;
+        }
+    }
+    k_delta_walk_back<In, DK, kIsLocal, 1><<<dim3(x, y, cols), 64, 0, a.stream>>>(
+        z, sg, a.d_o, a.d_hT, a.d_v, a.d_h0, ws);
 }
 
 // Starts of all segments: every segment walked from zero and from the
@@ -116,8 +147,7 @@ dim3 walk_grid(const Sizes& z, const Segments& sg, int cols) {
 template <typename In, int DK>
 void find_starts(const DeltaArgs& a, const Sizes& z, const Segments& sg, const Streams& ws) {
     const int tiles = z.dvp / 16;
-    k_delta_walk<In, DK, kLocal><<<walk_grid(z, sg, tiles + DK / 16), 64, 0, a.stream>>>(
-        z, sg, a.v, nullptr, nullptr, nullptr, ws);
+    walk<In, DK, kLocal>(a, z, sg, ws, tiles + DK / 16);
     const dim3 joint(static_cast<unsigned>(z.n_seq), static_cast<unsigned>(z.heads_v),
                      static_cast<unsigned>(tiles));
     k_delta_join<DK, false><<<joint, DK * 4, 0, a.stream>>>(z, sg, a.h0, ws);
@@ -128,8 +158,7 @@ void forward(const DeltaArgs& a, const Sizes& z, const Segments& sg, const Strea
     const dim3 chunks(static_cast<unsigned>(z.slots), static_cast<unsigned>(z.heads_v));
     k_delta_prepare<In, DK, false><<<chunks, 256, 0, a.stream>>>(z, a.q, a.k, a.g, a.beta, ws);
     if (sg.most > 1) find_starts<In, DK>(a, z, Segments{sg.most, sg.chunks, true}, ws);
-    k_delta_walk<In, DK, kOut><<<walk_grid(z, sg, z.dvp / 16), 64, 0, a.stream>>>(
-        z, sg, a.v, a.h0, a.o, a.hT, ws);
+    walk<In, DK, kOut>(a, z, sg, ws, z.dvp / 16);
 }
 
 template <typename In, int DK>
@@ -137,17 +166,14 @@ void backward(const DeltaArgs& a, const Sizes& z, const Segments& sg, const Stre
     const dim3 chunks(static_cast<unsigned>(z.slots), static_cast<unsigned>(z.heads_v));
     k_delta_prepare<In, DK, true><<<chunks, 256, 0, a.stream>>>(z, a.q, a.k, a.g, a.beta, ws);
     if (sg.most > 1) find_starts<In, DK>(a, z, sg, ws);
-    const dim3 grid = walk_grid(z, sg, z.dvp / 16);
-    k_delta_walk<In, DK, kSave><<<grid, 64, 0, a.stream>>>(z, sg, a.v, a.h0, nullptr, nullptr, ws);
+    walk<In, DK, kSave>(a, z, sg, ws, z.dvp / 16);
     if (sg.most > 1) {
-        k_delta_walk_back<In, DK, true><<<grid, 64, 0, a.stream>>>(
-            z, sg, a.d_o, nullptr, nullptr, nullptr, ws);
+        walk_back<In, DK, true>(a, z, sg, ws);
         const dim3 joint(static_cast<unsigned>(z.n_seq), static_cast<unsigned>(z.heads_v),
                          static_cast<unsigned>(z.dvp / 16));
         k_delta_join<DK, true><<<joint, DK * 4, 0, a.stream>>>(z, sg, a.d_hT, ws);
     }
-    k_delta_walk_back<In, DK, false><<<grid, 64, 0, a.stream>>>(z, sg, a.d_o, a.d_hT, a.d_v,
-                                                                a.d_h0, ws);
+    walk_back<In, DK, false>(a, z, sg, ws);
     const dim3 keys(static_cast<unsigned>(z.slots), static_cast<unsigned>(z.heads_k));
     k_delta_grads<In, DK><<<keys, 256, 0, a.stream>>>(z, a.d_o, a.d_q, a.d_k, a.g,
                                                       a.h0 == nullptr, a.d_g, a.d_beta, ws);

@@ -402,28 +402,46 @@ __device__ __forceinline__ bool part_of(const Sizes& z, const Segments& sg, Part
 }
 
 // One column of a chunk's 64 tokens, this lane's rows 16 t + 4 g + r: byte
-// offsets from the chunk's first token (sizes keep 64 tokens under 2 GiB).
+// offsets from the chunk's first token (sizes keep 64 tokens under 2 GiB), each
+// in a register, or (kLean) the first one alone and the others' distances in
+// scalar arithmetic.
+template <bool kLean>
 struct Column {
-    uint32_t at[kChunk / 16][4];
-    __device__ __forceinline__ Column(uint32_t stride, uint32_t g, uint32_t col, uint32_t size) {
+    uint32_t at[kLean ? 1 : kChunk / 16][4], pitch;
+    __device__ __forceinline__ Column(uint32_t stride, uint32_t g, uint32_t col, uint32_t size)
+        : pitch(stride * size) {
+        if constexpr (kLean) {
+            at[0][0] = (4 * g * stride + col) * size;
+        } else {
 #pragma unroll
-        for (int t = 0; t < kChunk / 16; ++t)
+            for (int t = 0; t < kChunk / 16; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) at[t][r] = ((16 * t + 4 * g + r) * stride + col) * size;
+                for (int r = 0; r < 4; ++r) at[t][r] = ((16 * t + 4 * g + r) * stride + col) * size;
+        }
+    }
+    template <typename B>
+    __device__ __forceinline__ B* row(B* base, int t, int r) const {
+        if constexpr (kLean) {
+            uint32_t step = pitch;
+            asm("" : "+s"(step));  // the products would be kept, each in a register
+            return base + (16 * t + r) * step + at[0][0];
+        } else {
+            return base + at[t][r];
+        }
     }
 };
 // Unconverted values (a conversion next to its load would make each load wait
 // for the last); left: tokens from the chunk's first to the sequence's end,
 // zeros behind it.
-template <typename In>
+template <typename In, bool kLean>
 __device__ __forceinline__ void load_column(In (&x)[kChunk / 16][4], const In* p,
-                                            const Column& c, int64_t left, int g) {
+                                            const Column<kLean>& c, int64_t left, int g) {
     const char* base = reinterpret_cast<const char*>(p);
     if (left >= kChunk) {
 #pragma unroll
         for (int t = 0; t < kChunk / 16; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) x[t][r] = *reinterpret_cast<const In*>(base + c.at[t][r]);
+            for (int r = 0; r < 4; ++r) x[t][r] = *reinterpret_cast<const In*>(c.row(base, t, r));
     } else {
 #pragma unroll
         for (int t = 0; t < kChunk / 16; ++t)
@@ -431,12 +449,12 @@ __device__ __forceinline__ void load_column(In (&x)[kChunk / 16][4], const In* p
             for (int r = 0; r < 4; ++r) {
                 x[t][r] = In{};
                 if (16 * t + 4 * g + r < left)
-                    x[t][r] = *reinterpret_cast<const In*>(base + c.at[t][r]);
+                    x[t][r] = *reinterpret_cast<const In*>(c.row(base, t, r));
             }
     }
 }
-template <typename In>
-__device__ __forceinline__ void store_column(In* p, const Column& c, const f32x4 (&x)[kChunk / 16],
+template <typename In, bool kLean>
+__device__ __forceinline__ void store_column(In* p, const Column<kLean>& c, const f32x4 (&x)[kChunk / 16],
                                              int64_t left, int g) {
     char* base = reinterpret_cast<char*>(p);
     if (left >= kChunk) {
@@ -444,14 +462,14 @@ __device__ __forceinline__ void store_column(In* p, const Column& c, const f32x4
         for (int t = 0; t < kChunk / 16; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                *reinterpret_cast<In*>(base + c.at[t][r]) = from_f32<In>(x[t][r]);
+                *reinterpret_cast<In*>(c.row(base, t, r)) = from_f32<In>(x[t][r]);
     } else {
 #pragma unroll
         for (int t = 0; t < kChunk / 16; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r)
                 if (16 * t + 4 * g + r < left)
-                    *reinterpret_cast<In*>(base + c.at[t][r]) = from_f32<In>(x[t][r]);
+                    *reinterpret_cast<In*>(c.row(base, t, r)) = from_f32<In>(x[t][r]);
     }
 }
 // Tiles of the workspace, padded rows pitch apart (at: this lane's first, bytes).
@@ -507,6 +525,44 @@ struct Scale {
     }
 };
 
+// Operands of a workgroup's W waves: up to three arrays of fragment planes and G
+// runs of four gates (a KiB each), of which every wave loads its share into registers and puts it into
+// LDS when the waves are done with what is there.
+template <int W, int A, int B, int D, int G>
+struct Shared {
+    static constexpr int kA = A, kB = B, kD = D, kUnits = A + B + D + G;
+    static constexpr int kEach = (kUnits + W - 1) / W;
+    f16x8 x[kEach];
+    __device__ __forceinline__ void load(const _Float16* a, const _Float16* b, const _Float16* d,
+                                         const float* gates, int wave, int lane) {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            int u = wave * kEach + i;
+            u = u < kUnits ? u : kUnits - 1;
+            const _Float16* p = u < A           ? a + u * 512
+                                : u < A + B     ? b + (u - A) * 512
+                                : u < A + B + D ? d + (u - A - B) * 512
+                                                : reinterpret_cast<const _Float16*>(gates) +
+                                                      (u - A - B - D) * 512;
+            x[i] = *reinterpret_cast<const f16x8*>(reinterpret_cast<const char*>(p) +
+                                                   static_cast<uint32_t>(lane) * 16);
+        }
+    }
+    __device__ __forceinline__ void put(_Float16* stage, int wave, int lane) const {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+            if (wave * kEach + i < kUnits)
+                *reinterpret_cast<f16x8*>(stage + (wave * kEach + i) * 512 + lane * 8) = x[i];
+    }
+};
+// Between the writes and the reads of LDS of a workgroup's waves. (Loads and
+// stores of memory go on.)
+__device__ __forceinline__ void share() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
 // The walks: a wave takes 16 columns of a head's state through the chunks of a
 // segment (a whole sequence, or a part of a long one) and shares nothing. The
 // operands of the next chunk are requested as soon as this one's are used. A
@@ -522,19 +578,20 @@ struct Scale {
 // takes any start through it.
 enum WalkKind { kOut, kSave, kLocal };
 
-template <typename In, int DK, WalkKind kKind>
-__global__ __launch_bounds__(64, 1) void k_delta_walk(const Sizes z, const Segments sg,
+template <typename In, int DK, WalkKind kKind, int W>
+__global__ __launch_bounds__(64 * W, W > 1 ? 2 : 1) void k_delta_walk(const Sizes z, const Segments sg,
                                                        const void* vp, const float* h0, void* op,
                                                        float* hT, const Streams ws) {
     constexpr int C = kChunk, NX = Planes<In>::kInput, NS = kPlanes;
     constexpr int NT = C / 16, KS = DK / 32, CS = C / 32, MT = DK / 16;
     // operands that fit the registers are requested a chunk ahead, others a
     // product or two
-    constexpr bool kAhead = DK * NX <= (kKind == kOut ? 64 : 128);
+    constexpr bool kShare = W > 1, kAhead = !kShare && DK * NX <= (kKind == kOut ? 64 : 128);
     Part part;
     if (!part_of(z, sg, part) || (kKind == kLocal && part.last && sg.skip_last)) return;
-    const int lane = threadIdx.x, g = lane / 16;
-    const int ct = blockIdx.z, tiles = z.dvp / 16;
+    const int lane = threadIdx.x % 64, g = lane / 16;
+    const int wave = W > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / 64) : 0;
+    const int ct = blockIdx.z * W + wave, tiles = z.dvp / 16;
     const int h = blockIdx.y, hk = h / z.group;
     const int col = ct * 16 + lane % 16;
     const bool on = col < z.dv;                           // a column of v
@@ -563,11 +620,12 @@ __global__ __launch_bounds__(64, 1) void k_delta_walk(const Sizes z, const Segme
     // lanes past the last column repeat the first one
     const In* v = static_cast<const In*>(vp) + part.start * z.v_stride + static_cast<int64_t>(h) * z.dv;
     In* o = static_cast<In*>(op) + part.start * step + static_cast<int64_t>(h) * z.dv;
-    const Column vc(static_cast<uint32_t>(z.v_stride), g, on ? col : 0, sizeof(In)),
+    const Column<kShare> vc(static_cast<uint32_t>(z.v_stride), g, on ? col : 0, sizeof(In)),
         oc(static_cast<uint32_t>(step), g, col, sizeof(In));
 
-    Frag<NX> ka[NT * KS], qa[kKind == kOut ? NT * KS : 1], kt[MT * CS];
-    Frag<NS> ta[kTri], pa[kKind == kOut ? kTri : 1];
+    Frag<NX> ka[kShare ? 1 : NT * KS], qa[!kShare && kKind == kOut ? NT * KS : 1],
+        kt[kShare ? 1 : MT * CS];
+    Frag<NS> ta[kShare ? 1 : kTri], pa[!kShare && kKind == kOut ? kTri : 1];
     In vr[NT][4] = {};
     f32x4 egk[NT], egq[NT], gu[NT];
     float last = 0.0f, psc = 0.0f, tsc = 0.0f;
@@ -579,29 +637,97 @@ __global__ __launch_bounds__(64, 1) void k_delta_walk(const Sizes z, const Segme
 #pragma unroll
         for (int t = 0; t < NT; ++t) x[t] = *reinterpret_cast<const f32x4*>(p + 64 * t + at);
     };
-    auto fetch_k = [&](int64_t ci) { fetch(ka, ws.KA + kbase(ci), lane); };
+    // K, Q and their gates; T, P, K^T and U's
+    constexpr int kUnitK = kEgK / 4, kUnitU = kU / 4;
+    static_assert(kEgQ / 4 == kUnitK + 1 && kChunk * 4 * 4 == 1024);
+    Shared<W, NT * KS * NX, kKind == kOut ? NT * KS * NX : 0, 0, kKind == kOut ? 2 : 1> first_ops;
+    Shared<W, kTri * NS, kKind == kOut ? kTri * NS : 0, MT * CS * NX, 1> then_ops;
+    __shared__ _Float16 stage[kShare ? (first_ops.kUnits + then_ops.kUnits) * 512 : 1];
+    _Float16* const then_stage = stage + (kShare ? first_ops.kUnits * 512 : 0);
+    auto load_first = [&](int64_t ci) {
+        first_ops.load(ws.KA + kbase(ci), ws.QA + kbase(ci), nullptr,
+                       ws.gates + (vslot(ci) * kGates + kUnitK * 4) * C, wave, lane);
+    };
+    auto load_then = [&](int64_t ci) {
+        then_ops.load(ws.TA + vslot(ci) * kTriSize * NS, ws.PA + vslot(ci) * kTriSize * NS,
+                      ws.KT + kbase(ci), ws.gates + (vslot(ci) * kGates + kUnitU * 4) * C, wave,
+                      lane);
+    };
+    auto staged = [&](const _Float16* at, int which, int t) {  // a gate's tile
+        return *reinterpret_cast<const f32x4*>(
+            reinterpret_cast<const char*>(at) + (which % 4 * C + 16 * t) * 4 +
+            static_cast<uint32_t>(g) * 16);
+    };
+    auto gate_k = [&](int t) {
+        if constexpr (kShare)
+            return staged(stage + (first_ops.kA + first_ops.kB) * 512, kEgK, t);
+        else return egk[t];
+    };
+    auto gate_q = [&](int t) {
+        if constexpr (kShare)
+            return staged(stage + (first_ops.kA + first_ops.kB + 1) * 512, kEgQ, t);
+        else return egq[t];
+    };
+    auto gate_u = [&](int t) {
+        if constexpr (kShare)
+            return staged(then_stage + (then_ops.kA + then_ops.kB + then_ops.kD) * 512, kU, t);
+        else return gu[t];
+    };
+    auto k_frag = [&](int i) {
+        if constexpr (kShare) return load_frag<NX>(stage, i, lane);
+        else return ka[i];
+    };
+    auto q_frag = [&](int i) {
+        if constexpr (kShare) return load_frag<NX>(stage + first_ops.kA * 512, i, lane);
+        else return qa[i];
+    };
+    auto t_frag = [&](int i) {
+        if constexpr (kShare) return load_frag<NS>(then_stage, i, lane);
+        else return ta[i];
+    };
+    auto p_frag = [&](int i) {
+        if constexpr (kShare) return load_frag<NS>(then_stage + then_ops.kA * 512, i, lane);
+        else return pa[i];
+    };
+    auto s_frag = [&](int i) {
+        if constexpr (kShare)
+            return load_frag<NX>(then_stage + (then_ops.kA + then_ops.kB) * 512, i, lane);
+        else return kt[i];
+    };
+    // reads of LDS stay with their products: the other wave of the SIMD has work
+    auto apart = [](int t) {
+        if (kShare && kKind == kOut && t % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+    };
+    auto fetch_k = [&](int64_t ci) {
+        if constexpr (!kShare) fetch(ka, ws.KA + kbase(ci), lane);
+    };
     auto fetch_v = [&](int64_t ci) {
         if (!blind) load_column(vr, v + ci * C * z.v_stride, vc, part.len - ci * C, g);
-        gate(ci, kEgK, egk);
+        if constexpr (!kShare) gate(ci, kEgK, egk);
     };
     auto fetch_t = [&](int64_t ci) {
-        fetch(ta, ws.TA + vslot(ci) * kTriSize * NS, lane);
+        if constexpr (!kShare) fetch(ta, ws.TA + vslot(ci) * kTriSize * NS, lane);
         tsc = ws.gates[(vslot(ci) * kGates + kT) * C];
     };
     auto fetch_q = [&](int64_t ci) {
-        fetch(qa, ws.QA + kbase(ci), lane);
-        gate(ci, kEgQ, egq);
+        if constexpr (!kShare) fetch(qa, ws.QA + kbase(ci), lane);
+        if constexpr (!kShare) gate(ci, kEgQ, egq);
     };
     auto fetch_p = [&](int64_t ci) {
-        fetch(pa, ws.PA + vslot(ci) * kTriSize * NS, lane);
+        if constexpr (!kShare) fetch(pa, ws.PA + vslot(ci) * kTriSize * NS, lane);
         psc = ws.gates[(vslot(ci) * kGates + kP) * C];
     };
     auto fetch_s = [&](int64_t ci) {
-        fetch(kt, ws.KT + kbase(ci), lane);
-        gate(ci, kU, gu);
+        if constexpr (!kShare) fetch(kt, ws.KT + kbase(ci), lane);
+        if constexpr (!kShare) gate(ci, kU, gu);
         last = ws.gates[(vslot(ci) * kGates + kEg) * C + C - 1];
     };
     if (part.c0 < part.c1) {
+        if constexpr (kShare) {
+            load_first(part.c0);
+            load_then(part.c0);
+            first_ops.put(stage, wave, lane);
+        }
         fetch_v(part.c0);
         fetch_k(part.c0);
         if constexpr (kAhead) {
@@ -624,6 +750,10 @@ __global__ __launch_bounds__(64, 1) void k_delta_walk(const Sizes z, const Segme
     }
     for (int64_t ci = part.c0; ci < part.c1; ++ci) {
         const int64_t next = ci + 1 < part.c1 ? ci + 1 : ci;
+        if constexpr (kShare) {
+            share();  // K and Q are there, T, P and K^T of the chunk before are used
+            load_first(next);
+        }
         float m = largest_of(S);
         if (Scale::over(m)) {
             const float f = s.fit(m);
@@ -642,10 +772,11 @@ __global__ __launch_bounds__(64, 1) void k_delta_walk(const Sizes z, const Segme
         f32x4 R[NT], O[NT];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
+            apart(t);
             f32x4 acc = {};
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) mma(acc, ka[t * KS + ks], sf[ks]);
-            acc *= egk[t];
+            for (int ks = 0; ks < KS; ++ks) mma(acc, k_frag(t * KS + ks), sf[ks]);
+            acc *= gate_k(t);
 #pragma unroll
             for (int r = 0; r < 4; ++r) R[t][r] = __builtin_fmaf(to_f32(vr[t][r]), s.up, -acc[r]);
         }
@@ -655,16 +786,18 @@ __global__ __launch_bounds__(64, 1) void k_delta_walk(const Sizes z, const Segme
         if constexpr (kKind == kOut) {
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
+                apart(t);
                 O[t] = f32x4{};
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) mma(O[t], qa[t * KS + ks], sf[ks]);
-                O[t] *= egq[t];
+                for (int ks = 0; ks < KS; ++ks) mma(O[t], q_frag(t * KS + ks), sf[ks]);
+                O[t] *= gate_q(t);
             }
             __builtin_amdgcn_sched_barrier(0);
             if constexpr (kAhead) fetch_q(next);
             else fetch_p(ci);
         }
         if constexpr (!kAhead) fetch_s(ci);
+        if constexpr (kShare) then_ops.put(then_stage, wave, lane);
         m = largest_of(R);
         auto rescale = [&](f32x4 (&x)[NT], float top) {  // the rest of what is held with it
             const float f = s.fit(top);
@@ -677,12 +810,17 @@ __global__ __launch_bounds__(64, 1) void k_delta_walk(const Sizes z, const Segme
         Frag<NS> rf[CS];
 #pragma unroll
         for (int cs = 0; cs < CS; ++cs) split<NS>(R[2 * cs], R[2 * cs + 1], 1.0f, rf[cs]);
+        if constexpr (kShare) {
+            share();  // T, P and K^T are there, K and Q are used
+            load_then(next);
+        }
         f32x4 E[NT];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
+            apart(t);
             E[t] = f32x4{};
 #pragma unroll
-            for (int cs = 0; cs <= t / 2; ++cs) mma(E[t], ta[lower_frag(t, cs)], rf[cs]);
+            for (int cs = 0; cs <= t / 2; ++cs) mma(E[t], t_frag(lower_frag(t, cs)), rf[cs]);
         }
         if (tsc != 1.0f) times(E, tsc);
         __builtin_amdgcn_sched_barrier(0);
@@ -699,8 +837,9 @@ __global__ __launch_bounds__(64, 1) void k_delta_walk(const Sizes z, const Segme
             const float down = psc * fast_rcp(s.up);  // the gates of Q hold P's scale
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
+                apart(t);
 #pragma unroll
-                for (int cs = 0; cs <= t / 2; ++cs) mma(O[t], pa[lower_frag(t, cs)], ef[cs]);
+                for (int cs = 0; cs <= t / 2; ++cs) mma(O[t], p_frag(lower_frag(t, cs)), ef[cs]);
                 O[t] *= down;
             }
             if (on) store_column(o + ci * C * step, oc, O, part.len - ci * C, g);
@@ -708,9 +847,10 @@ __global__ __launch_bounds__(64, 1) void k_delta_walk(const Sizes z, const Segme
             if constexpr (kAhead) fetch_p(next);
         }
         if constexpr (!kAhead) fetch_k(next);
+        if constexpr (kShare) first_ops.put(stage, wave, lane);
         // S = e^{G_C} S + K^T U, U = beta e^{G_C - G} E
 #pragma unroll
-        for (int t = 0; t < NT; ++t) E[t] *= gu[t];
+        for (int t = 0; t < NT; ++t) E[t] *= gate_u(t);
         times(S, last);
         m = __builtin_fmaxf(largest_of(E), largest_of(S));  // all that goes on
         if (Scale::over(m) || Scale::under(m)) {
@@ -722,9 +862,11 @@ __global__ __launch_bounds__(64, 1) void k_delta_walk(const Sizes z, const Segme
 #pragma unroll
         for (int cs = 0; cs < CS; ++cs) split<NS>(E[2 * cs], E[2 * cs + 1], 1.0f, uf[cs]);
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
+        for (int i = 0; i < MT; ++i) {
+            apart(i);
 #pragma unroll
-            for (int cs = 0; cs < CS; ++cs) mma(S[i], kt[i * CS + cs], uf[cs]);
+            for (int cs = 0; cs < CS; ++cs) mma(S[i], s_frag(i * CS + cs), uf[cs]);
+        }
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (kAhead) fetch_s(next);
     }
@@ -746,18 +888,19 @@ __global__ __launch_bounds__(64, 1) void k_delta_walk(const Sizes z, const Segme
 
 // The same columns' state gradients from the last chunk to the first. kIsLocal:
 // a segment's, from a zero end.
-template <typename In, int DK, bool kIsLocal>
-__global__ __launch_bounds__(64, 1) void k_delta_walk_back(const Sizes z, const Segments sg,
+template <typename In, int DK, bool kIsLocal, int W>
+__global__ __launch_bounds__(64 * W, W > 1 ? 2 : 1) void k_delta_walk_back(const Sizes z, const Segments sg,
                                                             const void* dop, const float* d_hT,
                                                             void* dvp, float* d_h0,
                                                             const Streams ws) {
     constexpr int C = kChunk, NX = Planes<In>::kInput, NS = kPlanes;
     constexpr int NT = C / 16, KS = DK / 32, CS = C / 32, MT = DK / 16;
-    constexpr bool kAhead = DK * NX <= 64;  // as in the forward walk
+    constexpr bool kShare = W > 1, kAhead = !kShare && DK * NX <= 64;  // as in the forward walk
     Part part;
     if (!part_of(z, sg, part) || (kIsLocal && part.first)) return;
-    const int lane = threadIdx.x, g = lane / 16;
-    const int ct = blockIdx.z;
+    const int lane = threadIdx.x % 64, g = lane / 16;
+    const int wave = W > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / 64) : 0;
+    const int ct = blockIdx.z * W + wave;
     const int h = blockIdx.y, hk = h / z.group;
     const int col = ct * 16 + lane % 16;
     const bool on = col < z.dv;
@@ -782,10 +925,10 @@ __global__ __launch_bounds__(64, 1) void k_delta_walk_back(const Sizes z, const 
     const int64_t first = part.start * step + static_cast<int64_t>(h) * z.dv;
     const In* dO = static_cast<const In*>(dop) + first;
     In* dV = static_cast<In*>(dvp) + first;
-    const Column oc(static_cast<uint32_t>(step), g, on ? col : 0, sizeof(In));
+    const Column<kShare> oc(static_cast<uint32_t>(step), g, on ? col : 0, sizeof(In));
 
-    Frag<NX> ka[NT * KS], kt[MT * CS], qt[MT * CS];
-    Frag<NS> pa[kTri], tt[kTri];
+    Frag<NX> ka[kShare ? 1 : NT * KS], kt[kShare ? 1 : MT * CS], qt[kShare ? 1 : MT * CS];
+    Frag<NS> pa[kShare ? 1 : kTri], tt[kShare ? 1 : kTri];
     In yr[NT][4] = {};
     f32x4 egk[NT], egq[NT], gu[NT];
     float last = 0.0f, psc = 0.0f, tsc = 0.0f;
@@ -797,28 +940,93 @@ __global__ __launch_bounds__(64, 1) void k_delta_walk_back(const Sizes z, const 
 #pragma unroll
         for (int t = 0; t < NT; ++t) x[t] = *reinterpret_cast<const f32x4*>(p + 64 * t + at);
     };
+    // K, P and the gates of U and Q; T, Q^T, K^T and the gates of K
+    constexpr int kUnitX = kU / 4, kUnitT = kEgK / 4;
+    static_assert(kEgQ / 4 == kUnitX);
+    Shared<W, NT * KS * NX, kTri * NS, 0, 1> first_ops;
+    Shared<W, kTri * NS, MT * CS * NX, MT * CS * NX, 1> then_ops;
+    __shared__ _Float16 stage[kShare ? (first_ops.kUnits + then_ops.kUnits) * 512 : 1];
+    _Float16* const then_stage = stage + (kShare ? first_ops.kUnits * 512 : 0);
+    auto load_first = [&](int64_t ci) {
+        first_ops.load(ws.KA + kbase(ci), ws.PA + vslot(ci) * kTriSize * NS, nullptr,
+                       ws.gates + (vslot(ci) * kGates + kUnitX * 4) * C, wave, lane);
+    };
+    auto load_then = [&](int64_t ci) {
+        then_ops.load(ws.TT + vslot(ci) * kTriSize * NS, ws.QT + kbase(ci), ws.KT + kbase(ci),
+                      ws.gates + (vslot(ci) * kGates + kUnitT * 4) * C, wave, lane);
+    };
+    auto staged = [&](const _Float16* at, int which, int t) {  // a gate's tile
+        return *reinterpret_cast<const f32x4*>(
+            reinterpret_cast<const char*>(at) + (which % 4 * C + 16 * t) * 4 +
+            static_cast<uint32_t>(g) * 16);
+    };
+    auto k_frag = [&](int i) {
+        if constexpr (kShare) return load_frag<NX>(stage, i, lane);
+        else return ka[i];
+    };
+    auto p_frag = [&](int i) {
+        if constexpr (kShare) return load_frag<NS>(stage + first_ops.kA * 512, i, lane);
+        else return pa[i];
+    };
+    auto gate_u = [&](int t) {
+        if constexpr (kShare) return staged(stage + (first_ops.kA + first_ops.kB) * 512, kU, t);
+        else return gu[t];
+    };
+    auto gate_q = [&](int t) {
+        if constexpr (kShare) return staged(stage + (first_ops.kA + first_ops.kB) * 512, kEgQ, t);
+        else return egq[t];
+    };
+    auto t_frag = [&](int i) {
+        if constexpr (kShare) return load_frag<NS>(then_stage, i, lane);
+        else return tt[i];
+    };
+    auto qt_frag = [&](int i) {
+        if constexpr (kShare) return load_frag<NX>(then_stage + then_ops.kA * 512, i, lane);
+        else return qt[i];
+    };
+    auto kt_frag = [&](int i) {
+        if constexpr (kShare)
+            return load_frag<NX>(then_stage + (then_ops.kA + then_ops.kB) * 512, i, lane);
+        else return kt[i];
+    };
+    auto gate_k = [&](int t) {
+        if constexpr (kShare)
+            return staged(then_stage + (then_ops.kA + then_ops.kB + then_ops.kD) * 512, kEgK, t);
+        else return egk[t];
+    };
     auto fetch_y = [&](int64_t ci) {
         load_column(yr, dO + ci * C * step, oc, part.len - ci * C, g);
     };
     auto fetch_x = [&](int64_t ci) {
-        fetch(ka, ws.KA + kbase(ci), lane);
-        fetch(pa, ws.PA + vslot(ci) * kTriSize * NS, lane);
-        gate(ci, kU, gu);
-        gate(ci, kEgQ, egq);
+        if constexpr (!kShare) {
+            fetch(ka, ws.KA + kbase(ci), lane);
+            fetch(pa, ws.PA + vslot(ci) * kTriSize * NS, lane);
+            gate(ci, kU, gu);
+            gate(ci, kEgQ, egq);
+        }
         psc = ws.gates[(vslot(ci) * kGates + kP) * C];
     };
     auto fetch_t = [&](int64_t ci) {
-        fetch(tt, ws.TT + vslot(ci) * kTriSize * NS, lane);
-        gate(ci, kEgK, egk);
+        if constexpr (!kShare) {
+            fetch(tt, ws.TT + vslot(ci) * kTriSize * NS, lane);
+            gate(ci, kEgK, egk);
+        }
         tsc = ws.gates[(vslot(ci) * kGates + kT) * C];
     };
     auto fetch_s = [&](int64_t ci) {
-        fetch(qt, ws.QT + kbase(ci), lane);
-        fetch(kt, ws.KT + kbase(ci), lane);
+        if constexpr (!kShare) {
+            fetch(qt, ws.QT + kbase(ci), lane);
+            fetch(kt, ws.KT + kbase(ci), lane);
+        }
         last = ws.gates[(vslot(ci) * kGates + kEg) * C + C - 1];
     };
     if (part.c0 < part.c1) {
         const int64_t ci = part.c1 - 1;
+        if constexpr (kShare) {
+            load_first(ci);
+            load_then(ci);
+            first_ops.put(stage, wave, lane);
+        }
         fetch_y(ci);
         fetch_x(ci);
         if constexpr (kAhead) {
@@ -837,6 +1045,10 @@ __global__ __launch_bounds__(64, 1) void k_delta_walk_back(const Sizes z, const 
     }
     for (int64_t ci = part.c1 - 1; ci >= part.c0; --ci) {
         const int64_t next = ci > part.c0 ? ci - 1 : ci;
+        if constexpr (kShare) {
+            share();  // K and P are there, T, Q^T and K^T of the chunk behind are used
+            load_first(next);
+        }
         f32x4 y[NT];
 #pragma unroll
         for (int t = 0; t < NT; ++t)
@@ -866,15 +1078,16 @@ __global__ __launch_bounds__(64, 1) void k_delta_walk_back(const Sizes z, const 
         for (int t = 0; t < NT; ++t) {
             f32x4 a = {}, b = {};
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) mma(a, ka[t * KS + ks], sf[ks]);
+            for (int ks = 0; ks < KS; ++ks) mma(a, k_frag(t * KS + ks), sf[ks]);
 #pragma unroll
-            for (int cs = t / 2; cs < CS; ++cs) mma(b, pa[upper_frag(t, cs)], yo[cs]);
-            X[t] = a * gu[t] + b * psc;
-            y[t] *= egq[t];
+            for (int cs = t / 2; cs < CS; ++cs) mma(b, p_frag(upper_frag(t, cs)), yo[cs]);
+            X[t] = a * gate_u(t) + b * psc;
+            y[t] *= gate_q(t);
         }
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (kAhead) fetch_x(next);
         else fetch_s(ci);
+        if constexpr (kShare) then_ops.put(then_stage, wave, lane);
         auto rescale = [&](f32x4 (&x)[NT], float top) {
             const float f = s.fit(top);
             times(x, f);
@@ -887,11 +1100,15 @@ __global__ __launch_bounds__(64, 1) void k_delta_walk_back(const Sizes z, const 
         Frag<NS> xf[CS];
 #pragma unroll
         for (int cs = 0; cs < CS; ++cs) split<NS>(X[2 * cs], X[2 * cs + 1], 1.0f, xf[cs]);
+        if constexpr (kShare) {
+            share();  // T, Q^T and K^T are there, K and P are used
+            load_then(next);
+        }
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             X[t] = f32x4{};
 #pragma unroll
-            for (int cs = t / 2; cs < CS; ++cs) mma(X[t], tt[upper_frag(t, cs)], xf[cs]);
+            for (int cs = t / 2; cs < CS; ++cs) mma(X[t], t_frag(upper_frag(t, cs)), xf[cs]);
         }
         if (tsc != 1.0f) times(X, tsc);
         if constexpr (!kIsLocal) {
@@ -903,9 +1120,10 @@ __global__ __launch_bounds__(64, 1) void k_delta_walk_back(const Sizes z, const 
             if (on) store_column(dV + ci * C * step, oc, d, part.len - ci * C, g);
         }
 #pragma unroll
-        for (int t = 0; t < NT; ++t) X[t] *= -egk[t];
+        for (int t = 0; t < NT; ++t) X[t] *= -gate_k(t);
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (kAhead) fetch_t(next);
+        if constexpr (kShare) first_ops.put(stage, wave, lane);
         times(S, last);
         m = __builtin_fmaxf(__builtin_fmaxf(largest_of(X), largest_of(y)), largest_of(S));
         if (Scale::over(m) || Scale::under(m)) rescale(X, m);
@@ -920,8 +1138,8 @@ __global__ __launch_bounds__(64, 1) void k_delta_walk_back(const Sizes z, const 
         for (int i = 0; i < MT; ++i) {
 #pragma unroll
             for (int cs = 0; cs < CS; ++cs) {
-                mma(S[i], qt[i * CS + cs], yf[cs]);
-                mma(S[i], kt[i * CS + cs], xf[cs]);
+                mma(S[i], qt_frag(i * CS + cs), yf[cs]);
+                mma(S[i], kt_frag(i * CS + cs), xf[cs]);
             }
         }
         __builtin_amdgcn_sched_barrier(0);

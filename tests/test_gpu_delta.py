@@ -197,6 +197,29 @@ def test_packed_long_and_short(dtype):
         check(a, b, name)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(48, 130, 1, 3, 128, 128), (48, 65, 3, 3, 104, 120),
+                                   (2, 9000, 1, 4, 128, 128)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_many_wide_states(shape, dtype):
+    """So many states of 128 rows that the waves of a workgroup share their
+    operands, whole sequences and segments, with partial chunks and columns."""
+    *x, h0 = make(*shape, dtype, seed=31)
+    if shape[1] > 1000:
+        x[3].mul_(0.05)
+    o, hT = forward(x, h0)
+    g = torch.Generator().manual_seed(3)
+    do = torch.randn(x[2].shape, generator=g).to(dtype).cuda()
+    dhT = torch.randn(h0.shape, generator=g).cuda()
+    got = backward(x, do, h0, dhT)
+    ro, rS = delta_ref(*x, 0.125, h0)
+    check(o, ro, "o")
+    check(hT, rS, "hT")
+    ref = delta_ref(*x, 0.125, h0, do=do, dhT=dhT)
+    for name, a, b in zip(("dq", "dk", "dv", "dg", "dbeta", "dh0"), got, ref):
+        check(a, b, name)
+
+
 @pytest.mark.parametrize("size", [1e-12, 1e12])
 def test_values_of_any_size(size):
     """Values and gradients far from 1, and one that is far from the rest."""
