@@ -103,43 +103,54 @@ Streams streams_of(void* ws, const Layout& o) {
     return s;
 }
 
-// A workgroup's waves: states of 128 rows in eights of tiles of columns share
-// their operands in LDS where there are more waves than one for each SIMD
-// (32 x 784 tokens, 6 heads of 128 x 128, 1536 waves: 157 us a forward call
-// against 204 with single waves; 8 x 784 tokens, 384 waves: 99 against 76).
-// Narrower states have work for few waves and lose (32 x 784 tokens, 6 heads of
-// 64 x 64, in fours: 96 against 83 us).
-bool in_eights(unsigned x, unsigned y, int cols) {
-    return cols % 8 == 0 && int64_t{x} * y * cols > 1024;
+// How a walk's waves, one to each tile of 16 columns of a head, are grouped.
+// More waves than one for each SIMD share their operands in LDS, in fours, or
+// eights of states of 128 rows; up to 512 forward waves hand their outputs to a
+// second one; those between stay alone. Calls, alone and so grouped, 784 tokens,
+// 6 heads, bf16: 64 sequences of 64 x 64 states (1536 waves) 237 and 168 us,
+// backward 788 and 632; 32 of 128 x 128 (1536) 204 and 157; 8 of 128 x 128 (384)
+// 76 and 99; 32 of 64 x 64 (768) in fours 83 and 96, in pairs 82 and 85; 8 of
+// 64 x 64 (192) in pairs 56 and 49.
+enum Grouping { kAlone, kPairs, kFours, kEights };
+template <int DK>
+Grouping grouping(const Sizes& z, const Segments& sg, int cols, bool out) {
+    const int64_t waves = z.n_seq * sg.most * z.heads_v * cols;
+    if (waves > 1024) {
+        if (DK == 128 && cols % 8 == 0) return kEights;
+        if (cols % 4 == 0) return kFours;
+    }
+    return out && DK < 128 && waves <= 512 ? kPairs : kAlone;
 }
 
 // A walk over cols tiles of columns.
 template <typename In, int DK, WalkKind kKind>
 void walk(const DeltaArgs& a, const Sizes& z, const Segments& sg, const Streams& ws, int cols) {
     const unsigned x = static_cast<unsigned>(z.n_seq * sg.most), y = static_cast<unsigned>(z.heads_v);
-    if constexpr (DK == 128) {
-        if (in_eights(x, y, cols)) {
-            k_delta_walk<In, DK, kKind, 8><<<dim3(x, y, cols / 8), 512, 0, a.stream>>>(
-                z, sg, a.v, a.h0, a.o, a.hT, ws);
-            return;
-        }
-    }
-    k_delta_walk<In, DK, kKind, 1><<<dim3(x, y, cols), 64, 0, a.stream>>>(z, sg, a.v, a.h0, a.o,
-                                                                       a.hT, ws);
+    const unsigned n = static_cast<unsigned>(cols);
+    auto go = [&](auto kernel, unsigned tiles, unsigned threads) {
+        kernel<<<dim3(x, y, n / tiles), threads, 0, a.stream>>>(z, sg, a.v, a.h0, a.o, a.hT, ws);
+    };
+    const Grouping by = grouping<DK>(z, sg, cols, kKind == kOut);
+    if constexpr (DK == 128)
+        if (by == kEights) return go(k_delta_walk<In, DK, kKind, 8>, 8, 512);
+    if constexpr (DK < 128 && kKind == kOut)
+        if (by == kPairs) return go(k_delta_walk<In, DK, kKind, 2>, 1, 128);
+    if (by == kFours) return go(k_delta_walk<In, DK, kKind, 4>, 4, 256);
+    go(k_delta_walk<In, DK, kKind, 1>, 1, 64);
 }
 template <typename In, int DK, bool kIsLocal>
 void walk_back(const DeltaArgs& a, const Sizes& z, const Segments& sg, const Streams& ws) {
     const unsigned x = static_cast<unsigned>(z.n_seq * sg.most), y = static_cast<unsigned>(z.heads_v);
     const int cols = z.dvp / 16;
-    if constexpr (DK == 128) {
-        if (in_eights(x, y, cols)) {
-            k_delta_walk_back<In, DK, kIsLocal, 8><<<dim3(x, y, cols / 8), 512, 0, a.stream>>>(
-                z, sg, a.d_o, a.d_hT, a.d_v, a.d_h0, ws);
-            return;
-        }
-    }
-    k_delta_walk_back<In, DK, kIsLocal, 1><<<dim3(x, y, cols), 64, 0, a.stream>>>(
-        z, sg, a.d_o, a.d_hT, a.d_v, a.d_h0, ws);
+    auto go = [&](auto kernel, unsigned tiles, unsigned threads) {
+        kernel<<<dim3(x, y, static_cast<unsigned>(cols) / tiles), threads, 0, a.stream>>>(
+            z, sg, a.d_o, a.d_hT, a.d_v, a.d_h0, ws);
+    };
+    const Grouping by = grouping<DK>(z, sg, cols, false);
+    if constexpr (DK == 128)
+        if (by == kEights) return go(k_delta_walk_back<In, DK, kIsLocal, 8>, 8, 512);
+    if (by == kFours) return go(k_delta_walk_back<In, DK, kIsLocal, 4>, 4, 256);
+    go(k_delta_walk_back<In, DK, kIsLocal, 1>, 1, 64);
 }
 
 // Starts of all segments: every segment walked from zero and from the

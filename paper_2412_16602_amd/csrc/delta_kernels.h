@@ -563,15 +563,114 @@ __device__ __forceinline__ void share() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+// Waves that a SIMD holds, which sets their registers.
+template <typename In, int DK, int W>
+constexpr int waves_a_simd() {
+    return W == 8 || (W == 4 && DK * Planes<In>::kInput <= 128) ||
+                   (W == 2 && Planes<In>::kInput == 1)
+               ? 2
+               : 1;
+}
+
+// What a wave that holds a state hands to the one that forms its outputs: the
+// state's operand before a chunk and the chunk's errors, each with its scale.
+template <int DK, int NT>
+struct Handed {
+    f16x8 state[DK / 32][kPlanes][64];
+    f32x4 errors[NT][64];
+    float up_state, up_errors;
+    __device__ __forceinline__ void put(const Frag<kPlanes> (&sf)[DK / 32], float up, int lane) {
+#pragma unroll
+        for (int ks = 0; ks < DK / 32; ++ks)
+#pragma unroll
+            for (int n = 0; n < kPlanes; ++n) state[ks][n][lane] = sf[ks].p[n];
+        up_state = up;
+    }
+    __device__ __forceinline__ void put(const f32x4 (&E)[NT], float up, int lane) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) errors[t][lane] = E[t];
+        up_errors = up;
+    }
+};
+
+// The outputs of a walk in pairs: O = scale e^G Q S + P diag(beta) E, a chunk
+// behind the wave that holds the state.
+template <typename In, int DK>
+__device__ __forceinline__ void walk_output(const Sizes& z, const Part& part, int h, int hk,
+                                            int col, int lane, const Handed<DK, kChunk / 16>* handed,
+                                            void* op, const Streams& ws) {
+    constexpr int C = kChunk, NX = Planes<In>::kInput, NS = kPlanes;
+    constexpr int NT = C / 16, KS = DK / 32, CS = C / 32;
+    const int g = lane / 16;
+    const bool on = col < z.dv;
+    const int64_t step = static_cast<int64_t>(z.heads_v) * z.dv;
+    In* o = static_cast<In*>(op) + part.start * step + static_cast<int64_t>(h) * z.dv;
+    const Column<NX == 1> oc(static_cast<uint32_t>(step), g, col, sizeof(In));
+    Frag<NX> qa[NT * KS];
+    Frag<NS> pa[kTri];
+    f32x4 egq[NT];
+    float psc = 0.0f;
+    auto vslot = [&](int64_t ci) { return (part.slot0 + ci) * z.heads_v + h; };
+    auto fetch_chunk = [&](int64_t ci) {
+        fetch(qa, ws.QA + ((part.slot0 + ci) * z.heads_k + hk) * C * DK * NX, lane);
+        fetch(pa, ws.PA + vslot(ci) * kTriSize * NS, lane);
+        const float* gates = ws.gates + vslot(ci) * kGates * C;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+            egq[t] = *reinterpret_cast<const f32x4*>(gates + kEgQ * C + 16 * t + 4 * g);
+        psc = gates[kP * C];
+    };
+    if (part.c0 < part.c1) fetch_chunk(part.c0);
+    for (int64_t ci = part.c0; ci < part.c1; ++ci) {
+        share();
+        const Handed<DK, NT>& in = handed[ci & 1];
+        const float up = in.up_errors, again = up * fast_rcp(in.up_state), down = psc * fast_rcp(up);
+        f32x4 O[NT], E[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            E[t] = in.errors[t][lane];
+            O[t] = f32x4{};
+        }
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            Frag<NS> sf;
+#pragma unroll
+            for (int n = 0; n < NS; ++n) sf.p[n] = in.state[ks][n][lane];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) mma(O[t], qa[t * KS + ks], sf);
+        }
+        Frag<NS> ef[CS];
+#pragma unroll
+        for (int cs = 0; cs < CS; ++cs) split<NS>(E[2 * cs], E[2 * cs + 1], 1.0f, ef[cs]);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            O[t] *= egq[t] * again;
+#pragma unroll
+            for (int cs = 0; cs <= t / 2; ++cs) mma(O[t], pa[lower_frag(t, cs)], ef[cs]);
+            O[t] *= down;
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        fetch_chunk(ci + 1 < part.c1 ? ci + 1 : ci);
+        if (on) store_column(o + ci * C * step, oc, O, part.len - ci * C, g);
+    }
+}
+
 // The walks: a wave takes 16 columns of a head's state through the chunks of a
-// segment (a whole sequence, or a part of a long one) and shares nothing. The
-// operands of the next chunk are requested as soon as this one's are used. A
-// chunk of 64 x 64 states takes about 450 vector instructions, 84 of them
-// matrix products, and 48 loads of a KiB; bound by that issue rate and, from
-// about four waves a compute unit on, by the 64 bytes a clock of L1. Measured:
-// 2.2 us a chunk. (Four waves a column tile, each a quarter of the rows, with
-// the tiles exchanged through LDS, took 1.7 times the instructions and twice
-// the time.)
+// segment (a whole sequence, or a part of a long one). W waves a workgroup:
+// - 1: it shares nothing, and requests the operands of the next chunk as soon
+//   as this one's are used. A chunk of 64 x 64 states takes about 450 vector
+//   instructions, 84 of them matrix products, and 48 loads of a KiB; bound by
+//   that issue rate and by the way through the chunk's dependent products, 2.2
+//   us a chunk (3.0 with outputs). (Four waves a column tile, each a quarter of
+//   the rows, with the tiles exchanged through LDS, took 1.7 times the
+//   instructions and twice the time.)
+// - 2: the state and the outputs are a wave each (walk_output), 2.1 us a chunk.
+// - 4, 8: neighbouring tiles' waves read their operands from LDS, where each
+//   has put its share of them, loaded a chunk ahead; two waves a SIMD then hide
+//   each other's latencies, and what comes through L1 is a fourth or an eighth
+//   (alone, 57 KB/us a compute unit bound them). 128 x 128 states: 7.3 us a
+//   chunk of eight tiles with outputs, alone 12; bound by instruction issue
+//   (636 vector instructions, 132 of them products, a chunk and wave).
 // kOut: write o and hT. kSave: keep each chunk's entry state and errors for the
 // backward pass. kLocal: a segment's end state from a zero start, and, in DK
 // further columns, from the identity without values, which is the matrix that
@@ -579,19 +678,20 @@ __device__ __forceinline__ void share() {
 enum WalkKind { kOut, kSave, kLocal };
 
 template <typename In, int DK, WalkKind kKind, int W>
-__global__ __launch_bounds__(64 * W, W > 1 ? 2 : 1) void k_delta_walk(const Sizes z, const Segments sg,
+__global__ __launch_bounds__(64 * W, (waves_a_simd<In, DK, W>())) void k_delta_walk(const Sizes z, const Segments sg,
                                                        const void* vp, const float* h0, void* op,
                                                        float* hT, const Streams ws) {
     constexpr int C = kChunk, NX = Planes<In>::kInput, NS = kPlanes;
     constexpr int NT = C / 16, KS = DK / 32, CS = C / 32, MT = DK / 16;
     // operands that fit the registers are requested a chunk ahead, others a
     // product or two
-    constexpr bool kShare = W > 1, kAhead = !kShare && DK * NX <= (kKind == kOut ? 64 : 128);
+    constexpr bool kShare = W > 2, kPair = W == 2, kOwn = kKind == kOut && !kPair;
+    constexpr bool kAhead = !kShare && DK * NX <= (kOwn ? 64 : 128);
     Part part;
     if (!part_of(z, sg, part) || (kKind == kLocal && part.last && sg.skip_last)) return;
     const int lane = threadIdx.x % 64, g = lane / 16;
     const int wave = W > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / 64) : 0;
-    const int ct = blockIdx.z * W + wave, tiles = z.dvp / 16;
+    const int ct = kPair ? blockIdx.z : blockIdx.z * W + wave, tiles = z.dvp / 16;
     const int h = blockIdx.y, hk = h / z.group;
     const int col = ct * 16 + lane % 16;
     const bool on = col < z.dv;                           // a column of v
@@ -601,6 +701,14 @@ __global__ __launch_bounds__(64 * W, W > 1 ? 2 : 1) void k_delta_walk(const Size
     const int64_t state = (part.seq * z.heads_v + h) * z.dk * z.dv + col;
     const uint32_t tile_at = static_cast<uint32_t>(4 * g * z.dvp + col) * 4;
 
+    using Seen = Handed<DK, NT>;
+    __shared__ Seen handed[kPair ? 2 : 1];
+    if constexpr (kPair) {
+        if (wave == 1) {
+            walk_output<In, DK>(z, part, h, hk, col, lane, handed, op, ws);
+            return;
+        }
+    }
     f32x4 S[MT];  // times scale.up, like R, E and U
 #pragma unroll
     for (int m = 0; m < MT; ++m)
@@ -620,12 +728,12 @@ __global__ __launch_bounds__(64 * W, W > 1 ? 2 : 1) void k_delta_walk(const Size
     // lanes past the last column repeat the first one
     const In* v = static_cast<const In*>(vp) + part.start * z.v_stride + static_cast<int64_t>(h) * z.dv;
     In* o = static_cast<In*>(op) + part.start * step + static_cast<int64_t>(h) * z.dv;
-    const Column<kShare> vc(static_cast<uint32_t>(z.v_stride), g, on ? col : 0, sizeof(In)),
+    const Column<kShare || (kPair && NX == 1)> vc(static_cast<uint32_t>(z.v_stride), g, on ? col : 0, sizeof(In)),
         oc(static_cast<uint32_t>(step), g, col, sizeof(In));
 
-    Frag<NX> ka[kShare ? 1 : NT * KS], qa[!kShare && kKind == kOut ? NT * KS : 1],
+    Frag<NX> ka[kShare ? 1 : NT * KS], qa[!kShare && kOwn ? NT * KS : 1],
         kt[kShare ? 1 : MT * CS];
-    Frag<NS> ta[kShare ? 1 : kTri], pa[!kShare && kKind == kOut ? kTri : 1];
+    Frag<NS> ta[kShare ? 1 : kTri], pa[!kShare && kOwn ? kTri : 1];
     In vr[NT][4] = {};
     f32x4 egk[NT], egq[NT], gu[NT];
     float last = 0.0f, psc = 0.0f, tsc = 0.0f;
@@ -732,7 +840,7 @@ __global__ __launch_bounds__(64 * W, W > 1 ? 2 : 1) void k_delta_walk(const Size
         fetch_k(part.c0);
         if constexpr (kAhead) {
             fetch_t(part.c0);
-            if constexpr (kKind == kOut) {
+            if constexpr (kOwn) {
                 fetch_q(part.c0);
                 fetch_p(part.c0);
             }
@@ -763,12 +871,13 @@ __global__ __launch_bounds__(64 * W, W > 1 ? 2 : 1) void k_delta_walk(const Size
             store_tiles(ws.S0 + vslot(ci) * DK * z.dvp, tile_at, z.dvp, S, on ? fast_rcp(s.up) : 0.0f);
         if constexpr (!kAhead) {
             fetch_t(ci);
-            if constexpr (kKind == kOut) fetch_q(ci);
+            if constexpr (kOwn) fetch_q(ci);
         }
         // R = V - e^G K S
         Frag<NS> sf[KS];
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) split<NS>(S[2 * ks], S[2 * ks + 1], 1.0f, sf[ks]);
+        if constexpr (kPair) handed[ci & 1].put(sf, s.up, lane);
         f32x4 R[NT], O[NT];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
@@ -783,7 +892,7 @@ __global__ __launch_bounds__(64 * W, W > 1 ? 2 : 1) void k_delta_walk(const Size
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (kAhead) fetch_k(next);
         fetch_v(next);
-        if constexpr (kKind == kOut) {
+        if constexpr (kOwn) {
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
                 apart(t);
@@ -803,7 +912,7 @@ __global__ __launch_bounds__(64 * W, W > 1 ? 2 : 1) void k_delta_walk(const Size
             const float f = s.fit(top);
             times(x, f);
             times(S, f);
-            if constexpr (kKind == kOut) times(O, f);
+            if constexpr (kOwn) times(O, f);
         };
         if (Scale::over(m)) rescale(R, m);
         // E = T R
@@ -827,10 +936,14 @@ __global__ __launch_bounds__(64 * W, W > 1 ? 2 : 1) void k_delta_walk(const Size
         if constexpr (kAhead) fetch_t(next);
         m = largest_of(E);
         if (Scale::over(m)) rescale(E, m);
+        if constexpr (kPair) {
+            handed[ci & 1].put(E, s.up, lane);
+            share();
+        }
         if constexpr (kKind == kSave)
             store_tiles(ws.E + vslot(ci) * C * z.dvp, tile_at, z.dvp, E, on ? fast_rcp(s.up) : 0.0f);
         // O = scale e^G Q S + P diag(beta) E
-        if constexpr (kKind == kOut) {
+        if constexpr (kOwn) {
             Frag<NS> ef[CS];
 #pragma unroll
             for (int cs = 0; cs < CS; ++cs) split<NS>(E[2 * cs], E[2 * cs + 1], 1.0f, ef[cs]);
@@ -889,7 +1002,7 @@ __global__ __launch_bounds__(64 * W, W > 1 ? 2 : 1) void k_delta_walk(const Size
 // The same columns' state gradients from the last chunk to the first. kIsLocal:
 // a segment's, from a zero end.
 template <typename In, int DK, bool kIsLocal, int W>
-__global__ __launch_bounds__(64 * W, W > 1 ? 2 : 1) void k_delta_walk_back(const Sizes z, const Segments sg,
+__global__ __launch_bounds__(64 * W, (waves_a_simd<In, DK, W>())) void k_delta_walk_back(const Sizes z, const Segments sg,
                                                             const void* dop, const float* d_hT,
                                                             void* dvp, float* d_h0,
                                                             const Streams ws) {

@@ -220,6 +220,26 @@ def test_many_wide_states(shape, dtype):
         check(a, b, name)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(96, 130, 1, 3, 64, 64), (96, 65, 3, 3, 32, 56),
+                                   (96, 70, 1, 3, 112, 64), (2, 9000, 1, 8, 48, 64)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_many_states(shape, dtype):
+    """As above with four tiles of columns, states of every padded height."""
+    *x, h0 = make(*shape, dtype, seed=37)
+    if shape[1] > 1000:
+        x[3].mul_(0.05)
+    o, hT = forward(x, h0)
+    do = torch.randn(x[2].shape, generator=torch.Generator().manual_seed(3)).to(dtype).cuda()
+    got = backward(x, do, h0, h0)
+    ro, rS = delta_ref(*x, 0.125, h0)
+    check(o, ro, "o")
+    check(hT, rS, "hT")
+    ref = delta_ref(*x, 0.125, h0, do=do, dhT=h0)
+    for name, a, b in zip(("dq", "dk", "dv", "dg", "dbeta", "dh0"), got, ref):
+        check(a, b, name)
+
+
 @pytest.mark.parametrize("size", [1e-12, 1e12])
 def test_values_of_any_size(size):
     """Values and gradients far from 1, and one that is far from the rest."""
