@@ -74,17 +74,30 @@ __device__ __forceinline__ constexpr int upper_frag(int t, int cs) {  // cs >= t
 // lower triangular I + M diag(beta): its 16 x 16 diagonal blocks by
 // substitution, a column to a lane, the blocks below by
 // -T_bb X_ba T_aa in binary32, first for pairs of blocks, then for pairs of pairs.
+// Bound by what it writes for the walks: 4704 slots of 64 x 64 states, backward,
+// 334 MB in 87 us (3.8 TB/s); 32 x 784 tokens, 6 heads, forward, 127 MB in 38 us.
+// More workgroups a compute unit (LDS used twice, 4 -> 5) gave 5 %, eight with
+// spilled registers lost 20 %.
+template <typename In, int DK>
+constexpr int prepare_workgroups() {  // of a compute unit, by LDS and registers
+    constexpr int wide = DK * Planes<In>::kInput;
+    return wide <= 64 ? 5 : wide <= 128 ? 4 : 2;
+}
 template <typename In, int DK, bool kBack>
-__global__ __launch_bounds__(256) void k_delta_prepare(const Sizes z, const void* qp,
+__global__ __launch_bounds__(256, (prepare_workgroups<In, DK>())) void k_delta_prepare(const Sizes z, const void* qp,
                                                        const void* kp, const float* gp,
                                                        const float* bp, const Streams ws) {
     constexpr int C = kChunk, NX = Planes<In>::kInput, NS = kPlanes;
     constexpr int NT = C / 16, KS = DK / 32, CS = C / 32, MT = DK / 16;
-    // rows of X: a pitch of 68 keeps 16-byte reads aligned and spreads the banks
-    __shared__ __align__(16) float X[C][C + 4];
+    // X takes the place of the fragments of K and Q when they are used. Its rows:
+    // a pitch of 68 keeps 16-byte reads aligned and spreads the banks.
+    constexpr int kFrags = NT * KS * NX * 512;
+    __shared__ __align__(16) _Float16 pool[2 * kFrags > C * (C + 4) * 2 ? 2 * kFrags
+                                                                    : C * (C + 4) * 2];
+    _Float16 *const kf = pool, *const qf = pool + kFrags;
+    float(*const X)[C + 4] = reinterpret_cast<float(*)[C + 4]>(pool);
     __shared__ __align__(16) float ghi[C], glo[C], sbeta[C], sk[C], sq[C];
     __shared__ float most_p[NT], most_t[NT];
-    __shared__ __align__(16) _Float16 kf[NT * KS * NX * 512], qf[NT * KS * NX * 512];
     const int64_t slot = blockIdx.x;
     const int h = blockIdx.y, hk = h / z.group;
     const Chunk c = chunk_of(z, slot);
@@ -202,7 +215,7 @@ __global__ __launch_bounds__(256) void k_delta_prepare(const Sizes z, const void
     // of tile t, columns j of tile w (P^T by rows). Everything above the
     // diagonal is set to 0 by a select.
     const float chi = ghi[mine], clo = glo[mine], cbeta = sbeta[mine];
-    f32x4 p[NT];
+    f32x4 p[NT], x[NT];
     float pm = 0.0f;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
@@ -224,7 +237,6 @@ __global__ __launch_bounds__(256) void k_delta_prepare(const Sizes z, const void
         const f32x4 rb = *reinterpret_cast<const f32x4*>(sbeta + a0);
         const f32x4 rk = *reinterpret_cast<const f32x4*>(sk + a0);
         const f32x4 rq = *reinterpret_cast<const f32x4*>(sq + a0);
-        f32x4 x;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int a = a0 + r;
@@ -234,14 +246,7 @@ __global__ __launch_bounds__(256) void k_delta_prepare(const Sizes z, const void
             const float pv = z.scale * (qk[r] * (kBack ? rq[r] * kcol : rk[r] * qcol)) * d * beta;
             const float xv = (kk[r] * (rk[r] * kcol)) * d * beta;
             p[t][r] = (kBack ? mine <= a : a <= mine) ? pv : 0.0f;
-            x[r] = (kBack ? mine < a : a < mine) ? xv : 0.0f;
-        }
-        // X by rows i: forward four neighbouring j of row mine
-        if constexpr (kBack) {
-#pragma unroll
-            for (int r = 0; r < 4; ++r) X[a0 + r][mine] = x[r];
-        } else {
-            *reinterpret_cast<f32x4*>(&X[mine][a0]) = x;
+            x[t][r] = (kBack ? mine < a : a < mine) ? xv : 0.0f;
         }
         pm = largest(pm, p[t]);
     }
@@ -257,7 +262,19 @@ __global__ __launch_bounds__(256) void k_delta_prepare(const Sizes z, const void
     };
     pm = over_wave(pm);
     if (lane == 0) most_p[w] = pm;
-    __syncthreads();
+    __syncthreads();  // K and Q are used
+    // X by rows i: forward four neighbouring j of row mine
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        if (kBack ? t < w : t > w) continue;
+        const int a0 = 16 * t + 4 * g;
+        if constexpr (kBack) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) X[a0 + r][mine] = x[t][r];
+        } else {
+            *reinterpret_cast<f32x4*>(&X[mine][a0]) = x[t];
+        }
+    }
     {
         // one scale for the chunk's P, which the forward walk's gates of Q share
         float m = most_p[0];
