@@ -452,7 +452,8 @@ vmb_status vmb_ss2d_out_norm(const void* y, const void* z, const float* gamma, c
  * 64) in that head, earlier ones included, and to all later ones of their
  * sequence; never to other sequences or heads.
  * Errors: VMB_ERR_NULL, VMB_ERR_SHAPE (sizes, strides, n_seq, scale not
- * finite), VMB_ERR_UNSUPPORTED (dk, dv), VMB_ERR_DTYPE, VMB_ERR_ALIGN (q, k, v,
+ * finite), VMB_ERR_UNSUPPORTED (dk, dv, more than 2^23 chunks or 2^22
+ * sequences), VMB_ERR_DTYPE, VMB_ERR_ALIGN (q, k, v,
  * o and the states 16 bytes, g, beta and cu_seqlens 4), VMB_ERR_ALIAS,
  * VMB_ERR_WORKSPACE.
  */
@@ -505,7 +506,7 @@ size_t vmb_gated_delta_workspace_bytes(int backward, int64_t batch, int64_t L, i
  *           n_slots is skipped: its o is set to 0 and no state is touched. No
  *           two rows may name the same slot.
  *   state : float32, [n_slots, heads_v, dk, dv]: read and written in place
- * Errors as for vmb_gated_delta_fwd (no workspace).
+ * Errors as for vmb_gated_delta_fwd (no workspace; at most 2^23 rows).
  */
 vmb_status vmb_gated_delta_step(const void* q, const void* k, const void* v, const float* g,
                                 const float* beta, const int32_t* slots, float* state, void* o,
@@ -582,10 +583,11 @@ typedef enum {
  *          NULL (1 and 0);  mean, rstd : float32, [batch, groups] (outputs), or
  *          both NULL
  *   eps >= 0, finite;  workspace : vmb_group_norm_act_workspace_bytes(0, ...)
- * Statistics in binary32: means and centred sums of squares of short runs,
- * joined pairwise, so an offset of the values does not cost accuracy.
+ * Statistics in binary32 from centred sums of squares, of values less one value
+ * of their group, so an offset of the values does not cost accuracy.
  * Errors: VMB_ERR_NULL, VMB_ERR_SHAPE (sizes, channels not a multiple of
- * groups, eps), VMB_ERR_UNSUPPORTED (act, more than 16384 channels),
+ * groups, eps), VMB_ERR_UNSUPPORTED (act, more than 16384 channels or 2^23
+ * groups of all images),
  * VMB_ERR_DTYPE, VMB_ERR_ALIGN (x, y, workspace 16 bytes; the rest 4),
  * VMB_ERR_ALIAS, VMB_ERR_WORKSPACE.
  */

@@ -8,6 +8,9 @@
 // over it before it is written back. Both contractions with the old state,
 // S^T k and S^T q, are summed in one exchange, because
 //   o = scale (a S^T q + (k . q) beta e).
+// 256 rows, 16 heads of 128 x 128, one token (540 MB): 87 us on one set of
+// states, partly from the last-level cache; 112 us on three in turn, 4.8 TB/s.
+// One row, 6 heads of 64 x 64, 4 tokens: 8 us, the launch and its latency.
 #include "vmb_internal.h"
 
 namespace vmb {
