@@ -543,8 +543,8 @@ struct Scale {
 };
 
 // Operands of a workgroup's W waves: up to three arrays of fragment planes and G
-// runs of four gates (a KiB each), of which every wave loads its share into registers and puts it into
-// LDS when the waves are done with what is there.
+// runs of four gates (a KiB each), of which every wave loads its share into
+// registers and puts it into LDS when the waves are done with what is there.
 template <int W, int A, int B, int D, int G>
 struct Shared {
     static constexpr int kA = A, kB = B, kD = D, kUnits = A + B + D + G;
@@ -1394,6 +1394,10 @@ __global__ __launch_bounds__(DK * 4) void k_delta_join(const Sizes z, const Segm
 // Columns of dv come 64 at a time: E, dR, dO and the state's rows are staged in
 // LDS as half-precision planes with one scale an array (found by the
 // workgroup from its registers), so each value is converted once.
+// 4704 chunks of 64 x 64 states, bf16 (about 590 MB read): 293 us; the same in
+// fp32 with 32 x 64 states, two value heads a key head, 616 chunks: 58 us. Bound
+// by the latencies of its steps at the two workgroups that registers and LDS
+// leave a compute unit, half of the memory's rate.
 constexpr int kVB = 64, kPitch = kVB + 8;
 
 template <int N>
