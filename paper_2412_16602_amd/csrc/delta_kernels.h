@@ -1396,8 +1396,10 @@ __global__ __launch_bounds__(DK * 4) void k_delta_join(const Sizes z, const Segm
 // workgroup from its registers), so each value is converted once.
 // 4704 chunks of 64 x 64 states, bf16 (about 590 MB read): 293 us; the same in
 // fp32 with 32 x 64 states, two value heads a key head, 616 chunks: 58 us. Bound
-// by the latencies of its steps at the two workgroups that registers and LDS
-// leave a compute unit, half of the memory's rate.
+// by its steps following each other at the two workgroups that registers and LDS
+// leave a compute unit: ended after the loads it takes 96 us, after the products
+// with dO, dR and the states 153, after the coefficients 203, after their
+// products 256. (Touching the late fragments early changed nothing.)
 constexpr int kVB = 64, kPitch = kVB + 8;
 
 template <int N>
